@@ -78,6 +78,9 @@ enum {
     SLIM_ERR_STATIC_SCRATCH = -7 /* slim_mpq_gemm_static: the shape needs more than the built-in scratch */
 };
 
+/* Element types of the calls that take more than one (a tensor's type is named by its argument). */
+enum { SLIM_F32 = 0, SLIM_F16 = 1, SLIM_BF16 = 2 };
+
 /* Library / format version: (SLIM_FORMAT_VERSION << 16) | build number. */
 int slim_version(void);
 /* Static, NUL-terminated description of a status code. */
@@ -405,6 +408,41 @@ int slim_gptq_factor(const void* x, int T, int K, double lambda, double* U_out, 
 int slim_gptq_quantize(const void* W, const void* x, const uint8_t* bits_host, double lambda, int use_sqc,
                        uint8_t* codes, void* scales, void* zeros, double* w_running,
                        int N, int K, int T, int g, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- distillation from a teacher's top logits ------------------------------------------------ */
+
+/* The error measure of SBA (softmax over the output features of each token, KL against the full-precision outputs; the
+ * appendix on the evaluation function) with a teacher of which only the k largest logits of every row are kept, and with its
+ * gradient with respect to the student's logits.  Per row t, with p = softmax(logits[t] / temperature) over the V columns and
+ * entries j = 0 .. k-1 (column index[t][j], teacher's logit value[t][j]):
+ *   teacher_lse == NULL: q = softmax(value / temperature) over the entries;  loss[t] = sum_j q_j (log q_j - log p_{index j})
+ *   otherwise teacher_lse[t] = log sum_v exp(teacher logit_v / temperature) over the teacher's whole row:
+ *     q_j = exp(value_j / temperature - teacher_lse), and all columns outside the entries are one more class with
+ *     q' = max(0, 1 - sum_j q_j) and p' = 1 - sum of p over the entries' columns: loss[t] += q' (log q' - log p')
+ *     (q' = 0 if there is no such column)
+ *   grad[t][v] = dloss[t] * d loss[t] / d logits[t][v]
+ * An entry whose index lies outside [0, V) is absent (padding: -1).  A row without a present entry, or (teacher_lse == NULL)
+ * whose present values are all minus infinity, has loss 0 and gradient 0, whatever its logits.  An index that occurs
+ * twice in a row is two entries of one column.  Logits of minus infinity have p = 0: with q > 0 there the loss is +infinity
+ * and the gradient finite; where the columns outside the entries have p' = 0 and q' > 0 their gradient is 0.  NaN, and
+ * logits of plus infinity, give NaN in their row alone.
+ *   logits  [M][V], row stride ld >= V elements, of SLIM_F32, SLIM_F16 or SLIM_BF16 (aligned to an element)
+ *   index   int32 or int64 (index_bytes 4 or 8) [M][k]; value [M][k] of any of the three types; teacher_lse, dloss, loss fp32 [M]
+ *   saved   fp32 [M][4], 16-byte aligned: what _grad needs of _loss (same logits, entries, teacher_lse and temperature); may be NULL in _loss
+ *   grad    [M][V] of the logits' type, row stride ldg >= V; may be the logits themselves (same pointer and stride)
+ * _step is _loss and _grad in one pass: it reads the logits once (V up to 262144, 131072 for fp32; beyond, twice).  Sums
+ * over the columns in fp32 and fp64, what is computed per entry in fp64; deterministic.  1 <= k <= SLIM_DISTILL_MAX_K,
+ * V <= SLIM_DISTILL_MAX_V, temperature > 0. */
+#define SLIM_DISTILL_MAX_K 1024
+#define SLIM_DISTILL_MAX_V 2097152
+int slim_distill_loss(const void* logits, int type, long long ld, const void* index, int index_bytes, const void* value, int value_type,
+                      const float* teacher_lse, double temperature, int M, int V, int k, float* loss, float* saved, void* stream);
+int slim_distill_grad(const void* logits, int type, long long ld, const void* index, int index_bytes, const void* value, int value_type,
+                      const float* teacher_lse, double temperature, int M, int V, int k, const float* saved, const float* dloss,
+                      void* grad, long long ldg, void* stream);
+int slim_distill_step(const void* logits, int type, long long ld, const void* index, int index_bytes, const void* value, int value_type,
+                      const float* teacher_lse, double temperature, int M, int V, int k, const float* dloss, float* loss,
+                      void* grad, long long ldg, void* stream);
 
 #ifdef __cplusplus
 }

@@ -43,7 +43,7 @@ def lib():
             raise RuntimeError(f"CUDA library not built: {LIB_PATH} is missing; run "
                                "`python -m paper_2405_14917_b200.build` (there is no CPU fallback)")
         L = ctypes.CDLL(LIB_PATH)
-        vp, i, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+        vp, i, ll, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_size_t
         L.slim_version.restype = i
         L.slim_version.argtypes = []
         L.slim_status_string.restype = ctypes.c_char_p
@@ -80,6 +80,9 @@ def lib():
             "slim_gptq_workspace_bytes": [i, i, i, i, ctypes.POINTER(sz)],
             "slim_gptq_factor": [vp, i, i, ctypes.c_double, vp, vp, vp, sz, vp],
             "slim_gptq_quantize": [vp, vp, vp, ctypes.c_double, i, vp, vp, vp, vp, i, i, i, i, vp, sz, vp],
+            "slim_distill_loss": [vp, i, ll, vp, i, vp, i, vp, ctypes.c_double, i, i, i, vp, vp, vp],
+            "slim_distill_grad": [vp, i, ll, vp, i, vp, i, vp, ctypes.c_double, i, i, i, vp, vp, vp, ll, vp],
+            "slim_distill_step": [vp, i, ll, vp, i, vp, i, vp, ctypes.c_double, i, i, i, vp, vp, vp, ll, vp],
         }
         for name, args in sigs.items():
             fn = getattr(L, name)
@@ -338,6 +341,115 @@ def softmax_kl(y_ref: torch.Tensor, y_q: torch.Tensor) -> torch.Tensor:
     _check("slim_softmax_kl", lib().slim_softmax_kl(_dev(y_ref, torch.float32, "y_ref"), _dev(y_q, torch.float16, "y_q"),
                                                     _dev(kl, torch.float64, "kl"), M, N, _stream(y_ref)))
     return kl
+
+
+_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}      # SLIM_F32, SLIM_F16, SLIM_BF16
+
+
+def _rows(t: torch.Tensor, name: str, dtypes, device=None) -> int:
+    """Row stride (elements) of a CUDA matrix whose rows are contiguous and do not overlap."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in dtypes):
+        raise TypeError(f"{name}: expected a CUDA matrix of dtype {' or '.join(str(d) for d in dtypes)}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, expected {device}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < cols:
+        raise ValueError(f"{name}: rows must be contiguous and must not overlap")
+    return t.stride(0) if rows > 1 else max(cols, 1)
+
+
+def _vector(t: torch.Tensor, n: int, dtype, name: str, device) -> int:
+    p = _dev(t, dtype, name)
+    if t.numel() != n or t.device != device:
+        raise ValueError(f"{name}: expected {n} elements on {device}")
+    return p
+
+
+class _device_of:
+    """The tensor's device as the current one, for calls that launch on it."""
+
+    def __init__(self, t: torch.Tensor):
+        self.index = t.device.index
+        self.back = None
+
+    def __enter__(self):
+        now = torch.cuda.current_device()
+        if now != self.index:
+            self.back = now
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *_):
+        if self.back is not None:
+            torch.cuda.set_device(self.back)
+
+
+def _distill_args(logits, top_index, top_logit, temperature, teacher_lse):
+    ld = _rows(logits, "logits", _TYPES)
+    M, V = logits.shape
+    if not (isinstance(top_index, torch.Tensor) and top_index.dtype in (torch.int32, torch.int64)):
+        raise TypeError("top_index: expected a contiguous CUDA tensor of dtype int32 or int64")
+    if not (isinstance(top_logit, torch.Tensor) and top_logit.dtype in _TYPES):
+        raise TypeError("top_logit: expected a contiguous CUDA tensor of dtype float32, float16 or bfloat16")
+    ip, vp = _dev(top_index, top_index.dtype, "top_index"), _dev(top_logit, top_logit.dtype, "top_logit")
+    if top_index.dim() != 2 or top_index.shape[0] != M or top_logit.shape != top_index.shape:
+        raise ValueError(f"top_index and top_logit must be [{M}][k]")
+    if top_index.device != logits.device or top_logit.device != logits.device:
+        raise ValueError(f"top_index and top_logit must be on {logits.device}")
+    lse = _vector(teacher_lse, M, torch.float32, "teacher_lse", logits.device) if teacher_lse is not None else None
+    return (logits.data_ptr(), _TYPES[logits.dtype], ld, ip, top_index.element_size(), vp, _TYPES[top_logit.dtype], lse, float(temperature),
+            M, V, top_index.shape[1])
+
+
+def _grad_out(logits, out):
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    ldg = _rows(out, "out", (logits.dtype,), logits.device)
+    if out.shape != logits.shape:
+        raise ValueError(f"out must be {tuple(logits.shape)}")
+    return out, ldg
+
+
+def distill_loss(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, temperature: float = 1.0,
+                 teacher_lse: torch.Tensor | None = None):
+    """KL of a teacher's top logits against softmax(logits / temperature) per row (slim_distill_loss): logits [M][V]
+    (fp32, fp16 or bf16, rows may be strided), top_index int32/int64 [M][k] (outside [0, V): absent), top_logit [M][k].
+    teacher_lse fp32 [M]: the log-sum-exp of the teacher's whole row / temperature, and then the columns outside
+    the entries count as one more class.  Returns (loss fp32 [M], saved), saved being what distill_grad needs."""
+    args = _distill_args(logits, top_index, top_logit, temperature, teacher_lse)
+    M = logits.shape[0]
+    loss = torch.empty(M, dtype=torch.float32, device=logits.device)
+    saved = torch.empty((M, 4), dtype=torch.float32, device=logits.device)
+    with _device_of(logits):
+        _check("slim_distill_loss", lib().slim_distill_loss(*args, loss.data_ptr(), saved.data_ptr(), _stream(logits)))
+    return loss, saved
+
+
+def distill_grad(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, saved: torch.Tensor, dloss: torch.Tensor,
+                 temperature: float = 1.0, teacher_lse: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of sum(dloss * loss) with respect to the logits, from what distill_loss saved for the same arguments
+    (slim_distill_grad).  dloss fp32 [M]; out may be the logits themselves."""
+    args = _distill_args(logits, top_index, top_logit, temperature, teacher_lse)
+    M = logits.shape[0]
+    sp = _vector(saved, 4 * M, torch.float32, "saved", logits.device)
+    dp = _vector(dloss, M, torch.float32, "dloss", logits.device)
+    out, ldg = _grad_out(logits, out)
+    with _device_of(logits):
+        _check("slim_distill_grad", lib().slim_distill_grad(*args, sp, dp, out.data_ptr(), ldg, _stream(logits)))
+    return out
+
+
+def distill_step(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch.Tensor, dloss: torch.Tensor, temperature: float = 1.0,
+                 teacher_lse: torch.Tensor | None = None, out: torch.Tensor | None = None):
+    """distill_loss and distill_grad in one pass over the logits, for a loss whose weights dloss (fp32 [M]) are known
+    beforehand (slim_distill_step).  Returns (loss fp32 [M], gradient); out may be the logits themselves."""
+    args = _distill_args(logits, top_index, top_logit, temperature, teacher_lse)
+    M = logits.shape[0]
+    dp = _vector(dloss, M, torch.float32, "dloss", logits.device)
+    out, ldg = _grad_out(logits, out)
+    loss = torch.empty(M, dtype=torch.float32, device=logits.device)
+    with _device_of(logits):
+        _check("slim_distill_step", lib().slim_distill_step(*args, dp, loss.data_ptr(), out.data_ptr(), ldg, _stream(logits)))
+    return loss, out
 
 
 def sba_workspace_bytes(M: int, N: int, K: int, avg_bits: int, g: int = GROUP) -> int:

@@ -1,0 +1,510 @@
+// slim_distill_loss / _grad / _step: distillation from a teacher's top logits, the KL of func SBA's error measure
+// (softmax over the output features of each token, Sec. 3.2.2) with a teacher of which only the k largest logits are kept, and its
+// gradient with respect to the student's logits.
+//
+// With p = softmax(s / T) over all V logits of a row, entries (i_j, u_j) and q_j the teacher's probabilities,
+//     loss   = sum_j q_j (log q_j - log p_{i_j})   [ + q' (log q' - log p') ],   q' = 1 - sum_j q_j, p' = 1 - sum of p over the set
+//     dloss/ds_v = (p_v * c - sum_{j: i_j = v} q_j) / T
+// without the rest q_j is the softmax over the entries and c = sum_j q_j; with it q_j = exp(u_j / T - lse), and c is
+// sum_j q_j + q' for the listed columns, that less q' / p' for all others.  So a row needs its maximum, its sum of exponentials
+// outside the listed columns, and k logits; then its gradient is one multiplication per element and k corrections.
+//
+// Bound: HBM (a row is read once, its gradient written once).  A row belongs to a cluster of 1 to 8 CTAs of 512 threads, each with
+// a slice of its columns; a thread takes eight 16-byte vectors of it at a time and, in the one-pass form, keeps them in registers
+// between the statistics and the gradient, so that the logits are not read again.  The slice statistics
+// meet through distributed shared memory; every sum has a fixed order.  Sums over the vocabulary are fp32 per thread (64 terms at a time) and fp64 from
+// there on; what is computed per row and per entry is fp64, because a small loss is the difference of large terms.
+#include "slim_gemv_dev.cuh"
+
+#include <cuda_bf16.h>
+
+#include <atomic>
+#include <cmath>
+
+namespace slim {
+
+constexpr int kDsThreads = 512;
+constexpr int kDsWarps = kDsThreads / 32;
+constexpr int kDsVecs = 8;                    // vectors of 16 bytes that a thread holds
+constexpr int kDsMaxCluster = 8;
+
+enum { kDsLoss = 0, kDsGrad = 1, kDsStep = 2 };
+
+struct DistillParams {
+    const void* logits;
+    const void* index;       // int32 or int64 [M][k]
+    const void* value;       // [M][k]
+    const float* lse;        // [M], or null: the teacher is renormalised over its entries
+    const float* dloss;      // [M]
+    float* loss;             // [M]
+    float* saved;            // [M][4]: the row's maximum, its sum of exponentials, that of the columns outside the set, 0
+    void* grad;
+    long long ld, ldg;       // row strides in elements
+    float c;                 // log2(e) / T
+    double inv_t;
+    int M, V, k;
+    int index64, value_type;
+    int ranks;               // CTAs of a row, a cluster
+    int slice;               // columns of a CTA
+    int mark_bytes;          // bytes of the set's marks (a byte per vector of the slice)
+};
+
+// ------------------------------------------------------------------------------------------ element types
+template <typename T> struct DsType;
+template <> struct DsType<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
+        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float* f) {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+    static __device__ __forceinline__ float one(float v) { return v; }
+    static __device__ __forceinline__ float round(float v) { return v; }
+};
+template <> struct DsType<__half> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            f[2 * i] = t.x; f[2 * i + 1] = t.y;
+        }
+    }
+    static __device__ __forceinline__ uint4 pack(const float* f) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ float one(__half v) { return __half2float(v); }
+    static __device__ __forceinline__ __half round(float v) { return __float2half_rn(v); }
+};
+template <> struct DsType<__nv_bfloat16> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ uint4 pack(const float* f) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    static __device__ __forceinline__ float one(__nv_bfloat16 v) { return __bfloat162float(v); }
+    static __device__ __forceinline__ __nv_bfloat16 round(float v) { return __float2bfloat16_rn(v); }
+};
+
+__device__ __forceinline__ float ex2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ double warp_sum(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ double warp_max(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// A slice of a row: its first column sits `shift` elements behind a 16-byte boundary, and vector j holds the columns
+// v0 - shift + j * E on; only the first and the last may reach past the slice, and are read and written by element.
+template <typename T>
+struct Slice {
+    const T* base;           // the 16-byte boundary
+    int shift, end, nv;      // elements [shift, end) from base belong to the slice
+    __device__ __forceinline__ Slice(const T* first, int n) {
+        constexpr int E = DsType<T>::E;
+        shift = static_cast<int>((reinterpret_cast<uintptr_t>(first) & 15u) / sizeof(T));
+        base = first - shift;
+        end = shift + n;
+        nv = n > 0 ? (end + E - 1) / E : 0;
+    }
+    __device__ __forceinline__ bool whole(int j) const {
+        constexpr int E = DsType<T>::E;
+        return j * E >= shift && (j + 1) * E <= end;
+    }
+    // Columns outside the slice read as minus infinity: they take no part in the maximum or the sum.
+    __device__ __forceinline__ uint4 load(int j) const {
+        constexpr int E = DsType<T>::E;
+        if (j < nv && whole(j)) return __ldcs(reinterpret_cast<const uint4*>(base) + j);
+        float f[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = j * E + e;
+            f[e] = j < nv && i >= shift && i < end ? DsType<T>::one(base[i]) : -INFINITY;
+        }
+        return DsType<T>::pack(f);
+    }
+};
+
+template <typename T, bool REST, int MODE>
+__global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillParams p) {
+    constexpr int E = DsType<T>::E;
+    extern __shared__ __align__(16) unsigned char ds_smem[];
+    double* s_q = reinterpret_cast<double*>(ds_smem);                  // [k] teacher's probability
+    double* s_lq = s_q + p.k;                                          // [k] its logarithm
+    int* s_idx = reinterpret_cast<int*>(s_lq + p.k);                   // [k] column, -1 where the entry is absent
+    float* s_s = reinterpret_cast<float*>(s_idx + p.k);                // [k] student's logit
+    uint8_t* s_first = reinterpret_cast<uint8_t*>(s_s + p.k);          // [k] no entry before it has this column
+    uint32_t* s_mark = reinterpret_cast<uint32_t*>(ds_smem + ((25 * p.k + 15) & ~15));    // REST: bit e of byte j: element e of vector j is listed
+    __shared__ float s_max[kDsWarps];
+    __shared__ double s_sum[kDsWarps];
+    __shared__ float2 s_slice;                                         // maximum and sum of this slice, for the cluster
+    __shared__ double s_row[8];
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int ranks = p.ranks;
+    const int row = static_cast<int>(blockIdx.x) / ranks, rank = static_cast<int>(blockIdx.x) - row * ranks;
+    const int v0 = min(p.V, rank * p.slice), v1 = min(p.V, v0 + p.slice);
+    const T* r_logits = static_cast<const T*>(p.logits) + static_cast<long long>(row) * p.ld;
+    const Slice<T> sl(r_logits + v0, v1 - v0);
+
+    uint4 x[kDsVecs];
+#pragma unroll
+    for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(tid + u * kDsThreads);
+
+    // ---- the entries: columns, the teacher's values, the student's logits at them
+    for (int j = tid; j < p.k; j += kDsThreads) {
+        const size_t at = static_cast<size_t>(row) * p.k + j;
+        const long long i = p.index64 ? static_cast<const long long*>(p.index)[at] : static_cast<const int*>(p.index)[at];
+        const bool in = i >= 0 && i < p.V;
+        double u;
+        if (p.value_type == SLIM_F32) u = static_cast<const float*>(p.value)[at];
+        else if (p.value_type == SLIM_F16) u = __half2float(static_cast<const __half*>(p.value)[at]);
+        else u = __bfloat162float(static_cast<const __nv_bfloat16*>(p.value)[at]);
+        s_idx[j] = in ? static_cast<int>(i) : -1;
+        s_s[j] = in ? DsType<T>::one(r_logits[i]) : 0.f;
+        s_lq[j] = u * p.inv_t;
+    }
+    if (REST)
+        for (int j = tid; j < p.mark_bytes / 4; j += kDsThreads) s_mark[j] = 0u;
+    __syncthreads();
+    for (int j = tid; j < p.k; j += kDsThreads) {
+        const int i = s_idx[j];
+        bool first = i >= 0;
+        for (int o = 0; o < j; ++o) first = first && s_idx[o] != i;
+        s_first[j] = first;
+        if (REST && i >= v0 && i < v1) {
+            const int e = i - v0 + sl.shift;
+            atomicOr(s_mark + (e / E >> 2), 1u << ((e / E & 3) * 8 + e % E));
+        }
+    }
+    if (warp == 0) {
+        // the teacher's probabilities; a row has something to learn from if an entry is present (and, without the rest, not all of them are minus infinity)
+        double top = -INFINITY;
+        int any = 0, finite = 0;
+        for (int j = lane; j < p.k; j += 32)
+            if (s_idx[j] >= 0) { top = fmax(top, s_lq[j]); any = 1; finite |= !(s_lq[j] == -INFINITY); }
+        any = __any_sync(0xffffffffu, any);
+        finite = __any_sync(0xffffffffu, finite);
+        double norm;
+        if (REST) norm = p.lse[row];
+        else {
+            top = warp_max(top);
+            any = finite;
+            double sum = 0.0;
+            for (int j = lane; j < p.k; j += 32)
+                if (s_idx[j] >= 0) sum += exp(s_lq[j] - top);
+            norm = top + log(warp_sum(sum));
+        }
+        double q_sum = 0.0;
+        for (int j = lane; j < p.k; j += 32) {
+            const double lq = s_lq[j] - norm;
+            const double q = s_idx[j] >= 0 && any ? exp(lq) : 0.0;
+            s_lq[j] = lq;
+            s_q[j] = q;
+            q_sum += q;
+        }
+        q_sum = warp_sum(q_sum);
+        if (lane == 0) { s_row[0] = q_sum; s_row[1] = any; }
+    }
+    __syncthreads();
+
+    // ---- the row's maximum and sum of exponentials, of the columns outside the set with REST
+    float m;
+    double R;                                        // sum over the columns (outside the set) of 2^((s - m) c)
+    const uint8_t* mark = reinterpret_cast<const uint8_t*>(s_mark);
+    if (MODE != kDsGrad) {
+        float tm = -INFINITY, ts = 0.f;
+        for (int j0 = 0; j0 < sl.nv; j0 += kDsVecs * kDsThreads) {
+            if (j0 > 0) {
+#pragma unroll
+                for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(j0 + tid + u * kDsThreads);
+            }
+            float cm = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kDsVecs; ++u) {
+                float f[E];
+                DsType<T>::unpack(x[u], f);
+#pragma unroll
+                for (int e = 0; e < E; ++e) cm = fmaxf(cm, f[e]);
+            }
+            if (cm > tm) { ts *= tm == -INFINITY ? 0.f : ex2((tm - cm) * p.c); tm = cm; }
+            const float ref = tm == -INFINITY ? 0.f : tm;
+#pragma unroll
+            for (int u = 0; u < kDsVecs; ++u) {
+                float f[E];
+                DsType<T>::unpack(x[u], f);
+                const int j = j0 + tid + u * kDsThreads;
+                if (REST && j < sl.nv) {
+                    const uint32_t b = mark[j];
+                    if (b != 0) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (b >> e & 1u) f[e] = -INFINITY;
+                    }
+                }
+                float s = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) s += ex2((f[e] - ref) * p.c);
+                ts += s;
+            }
+        }
+        float wm = tm;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
+        if (lane == 0) s_max[warp] = wm;
+        __syncthreads();
+        m = s_max[0];
+#pragma unroll
+        for (int w = 1; w < kDsWarps; ++w) m = fmaxf(m, s_max[w]);
+        const double ws = warp_sum(tm == -INFINITY ? static_cast<double>(ts) : static_cast<double>(ts * ex2((tm - m) * p.c)));
+        if (lane == 0) s_sum[warp] = ws;
+        __syncthreads();
+        R = 0.0;
+#pragma unroll
+        for (int w = 0; w < kDsWarps; ++w) R += s_sum[w];
+        if (ranks > 1) {
+            if (tid == 0) s_slice = make_float2(m, static_cast<float>(R));
+            cluster_sync_all();
+            const uint32_t at = smem_u32(&s_slice);
+            float mm = -INFINITY;
+            for (int r = 0; r < ranks; ++r) mm = fmaxf(mm, ld_cluster_f32x2(at, r).x);
+            R = 0.0;
+            for (int r = 0; r < ranks; ++r) {
+                const float2 o = ld_cluster_f32x2(at, r);
+                R += o.x == -INFINITY ? static_cast<double>(o.y) : static_cast<double>(o.y) * static_cast<double>(ex2((o.x - mm) * p.c));
+            }
+            m = mm;
+        }
+    } else {
+        const float4 sv = *reinterpret_cast<const float4*>(p.saved + 4 * static_cast<size_t>(row));
+        m = sv.x;
+        R = REST ? sv.z : sv.y;
+        if (ranks > 1) cluster_sync_all();           // grad may be logits: every CTA of the row has its entries' logits
+    }
+
+    // ---- what the row comes to: by warp 0, in 64 bits
+    if (warp == 0) {
+        const double ln2 = 0.69314718055994530942, cd = p.c, md = m == -INFINITY ? 0.0 : static_cast<double>(m);
+        double Z = R;
+        if (REST) {
+            double z = 0.0;
+            for (int j = lane; j < p.k; j += 32)
+                if (s_first[j]) z += exp((static_cast<double>(s_s[j]) - md) * cd * ln2);
+            Z += warp_sum(z);
+        }
+        if (MODE == kDsGrad) Z = p.saved[4 * static_cast<size_t>(row) + 1];
+        const double lz = log(Z), q_sum = s_row[0];
+        const bool any = s_row[1] != 0.0;
+        double l = 0.0, p_in = 0.0;
+        int columns = 0;
+        for (int j = lane; j < p.k; j += 32) {
+            if (s_idx[j] < 0) continue;
+            const double lp = Z == 0.0 ? -INFINITY : (static_cast<double>(s_s[j]) - md) * cd * ln2 - lz;
+            if (!(s_q[j] == 0.0)) l += s_q[j] * (s_lq[j] - lp);
+            if (REST && s_first[j]) { p_in += exp(lp); ++columns; }
+        }
+        l = warp_sum(l);
+        double mass = q_sum, other = q_sum;          // factor of p_v in the gradient of the listed columns, of the others
+        if (REST) {
+            p_in = warp_sum(p_in);
+            // the mass outside the set: what the listed columns leave of 1, unless that would cancel
+            const bool little = p_in < 0.5;
+            const double p_rest = Z == 0.0 ? 0.0 : little ? 1.0 - p_in : R / Z;
+            const bool others = __reduce_add_sync(0xffffffffu, columns) < p.V;
+            const double q_rest = others ? fmax(1.0 - q_sum, 0.0) : 0.0;
+            mass = q_sum + q_rest;
+            other = mass;
+            if (q_rest > 0.0) {
+                l += q_rest * (log(q_rest) - (p_rest == 0.0 ? -INFINITY : little ? log1p(-p_in) : log(p_rest)));
+                other = p_rest == 0.0 ? 0.0 : mass - q_rest / p_rest;
+            }
+            if (q_sum != q_sum) mass = other = l = q_sum;          // a NaN among the teacher's values
+        }
+        if (lane == 0) {
+            if (MODE != kDsGrad && rank == 0) {
+                p.loss[row] = any ? static_cast<float>(l) : 0.f;
+                if (MODE == kDsLoss && p.saved != nullptr)
+                    *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) =
+                        make_float4(m, static_cast<float>(Z), static_cast<float>(R), 0.f);
+            }
+            if (MODE != kDsLoss) {
+                const double d = static_cast<double>(p.dloss[row]) * p.inv_t;
+                s_row[2] = mass * d;
+                s_row[3] = Z == 0.0 ? 0.0 : other * d / Z;
+                s_row[4] = Z == 0.0 ? 0.0 : 1.0 / Z;
+                s_row[5] = d;
+            }
+        }
+    }
+    if (MODE == kDsLoss) {
+        if (ranks > 1) cluster_sync_all();           // the others may still read this CTA's slice statistics
+        return;
+    }
+    __syncthreads();
+
+    // ---- the gradient: one factor for the whole row, then the listed columns
+    const bool any = s_row[1] != 0.0;
+    const float ref = m == -INFINITY ? 0.f : m;
+    const float factor = any ? static_cast<float>(s_row[3]) : 0.f;
+    T* r_grad = static_cast<T*>(p.grad) + static_cast<long long>(row) * p.ldg;
+    T* g_base = r_grad + v0 - sl.shift;
+    const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
+    for (int j0 = 0; j0 < sl.nv; j0 += kDsVecs * kDsThreads) {
+        if (sl.nv > kDsVecs * kDsThreads) {          // more than the registers hold: read again
+#pragma unroll
+            for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(j0 + tid + u * kDsThreads);
+        }
+#pragma unroll
+        for (int u = 0; u < kDsVecs; ++u) {
+            const int j = j0 + tid + u * kDsThreads;
+            if (j >= sl.nv) break;
+            float f[E];
+            DsType<T>::unpack(x[u], f);
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[e] = any ? ex2((f[e] - ref) * p.c) * factor : 0.f;
+            if (vectors && sl.whole(j)) __stcs(reinterpret_cast<uint4*>(g_base) + j, DsType<T>::pack(f));
+            else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const int i = j * E + e;
+                    if (i >= sl.shift && i < sl.end) g_base[i] = DsType<T>::round(f[e]);
+                }
+            }
+        }
+    }
+    __syncthreads();                                 // the listed columns are written over
+    if (any) {
+        const double ln2 = 0.69314718055994530942, cd = p.c, md = m == -INFINITY ? 0.0 : static_cast<double>(m);
+        for (int j = tid; j < p.k; j += kDsThreads) {
+            const int i = s_idx[j];
+            if (!s_first[j] || i < v0 || i >= v1) continue;
+            double q = 0.0;
+            for (int o = j; o < p.k; ++o) q += s_idx[o] == i ? s_q[o] : 0.0;
+            const double e = exp((static_cast<double>(s_s[j]) - md) * cd * ln2);
+            r_grad[i] = DsType<T>::round(static_cast<float>(e * s_row[4] * s_row[2] - q * s_row[5]));
+        }
+    }
+    if (MODE == kDsStep && ranks > 1) cluster_sync_all();
+}
+
+// ------------------------------------------------------------------------------------------ host side
+template <typename T, bool REST, int MODE>
+static cudaError_t distill_launch_as(const DistillParams& p, int cluster, size_t smem, cudaStream_t s) {
+    static std::atomic<bool> attr_set[64];    // zero-initialised; set-up is idempotent, so a race repeats it harmlessly
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+        e = cudaFuncSetAttribute(distill_kernel<T, REST, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 104 * 1024);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(static_cast<unsigned>(p.M) * cluster, 1, 1);
+    cfg.blockDim = dim3(kDsThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = static_cast<unsigned>(cluster); attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, distill_kernel<T, REST, MODE>, p);
+}
+template <typename T, int MODE>
+static cudaError_t distill_launch_rest(const DistillParams& p, int cluster, size_t smem, cudaStream_t s) {
+    return p.lse != nullptr ? distill_launch_as<T, true, MODE>(p, cluster, smem, s) : distill_launch_as<T, false, MODE>(p, cluster, smem, s);
+}
+template <int MODE>
+static cudaError_t distill_launch(const DistillParams& p, int type, int cluster, size_t smem, cudaStream_t s) {
+    switch (type) {
+        case SLIM_F32: return distill_launch_rest<float, MODE>(p, cluster, smem, s);
+        case SLIM_F16: return distill_launch_rest<__half, MODE>(p, cluster, smem, s);
+        default: return distill_launch_rest<__nv_bfloat16, MODE>(p, cluster, smem, s);
+    }
+}
+
+static bool known_type(int t) { return t == SLIM_F32 || t == SLIM_F16 || t == SLIM_BF16; }
+static bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+static int distill(int mode, const void* logits, int type, long long ld, const void* index, int index_bytes, const void* value, int value_type,
+                   const float* lse, double temperature, int M, int V, int k, float* loss, float* saved, const float* dloss, void* grad,
+                   long long ldg, void* stream) {
+    if (M < 0 || V < 1 || k < 1 || !known_type(type) || !known_type(value_type) || (index_bytes != 4 && index_bytes != 8)) return SLIM_ERR_INVALID_ARG;
+    if (!(temperature > 0.0) || !(temperature <= 1e30) || !(temperature >= 1e-30) || ld < V || (mode != kDsLoss && ldg < V)) return SLIM_ERR_INVALID_ARG;
+    if (V > SLIM_DISTILL_MAX_V || k > SLIM_DISTILL_MAX_K || M > (1 << 27)) return SLIM_ERR_UNSUPPORTED;
+    if (M == 0) return SLIM_OK;
+    if (logits == nullptr || index == nullptr || value == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (mode != kDsGrad && loss == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (mode != kDsLoss && (dloss == nullptr || grad == nullptr)) return SLIM_ERR_INVALID_ARG;
+    if (mode == kDsGrad && saved == nullptr) return SLIM_ERR_INVALID_ARG;
+    const int es = type == SLIM_F32 ? 4 : 2;
+    if (!aligned_to(logits, es) || !aligned_to(grad, es) || !aligned_to(index, index_bytes) || !aligned_to(value, value_type == SLIM_F32 ? 4 : 2) ||
+        !aligned_to(lse, 4) || !aligned_to(dloss, 4) || !aligned_to(loss, 4) || !aligned16(saved))
+        return SLIM_ERR_ALIGNMENT;
+    const int E = 16 / es, held = kDsThreads * kDsVecs;            // vectors that a CTA's registers hold
+    // A cluster as large as the one pass needs to hold a row, or as fills the SMs twice while a thread still has a vector.
+    const int vecs = V / E + 2;
+    int cluster = 1;
+    while (cluster < kDsMaxCluster && ((mode == kDsStep && vecs > cluster * (held - 1)) || vecs > cluster * 65536 / 2 ||
+                                       (static_cast<long long>(M) * cluster < 2 * device_sm_count() && vecs > cluster * kDsThreads)))
+        cluster *= 2;
+    DistillParams p;
+    memset(&p, 0, sizeof p);
+    p.logits = logits; p.index = index; p.value = value; p.lse = lse; p.dloss = dloss; p.loss = loss; p.saved = saved; p.grad = grad;
+    p.ld = ld; p.ldg = ldg;
+    p.c = static_cast<float>(1.44269504088896340736 / temperature);
+    p.inv_t = 1.0 / temperature;
+    p.M = M; p.V = V; p.k = k;
+    p.index64 = index_bytes == 8;
+    p.value_type = value_type;
+    p.ranks = cluster;
+    p.slice = ((V + cluster - 1) / cluster + E - 1) / E * E;
+    p.mark_bytes = lse != nullptr ? (p.slice / E + 1 + 3) / 4 * 4 : 0;
+    const size_t smem = ((25 * static_cast<size_t>(k) + 15) & ~static_cast<size_t>(15)) + p.mark_bytes;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    SLIM_CUDA_TRY(mode == kDsLoss ? distill_launch<kDsLoss>(p, type, cluster, smem, s)
+                  : mode == kDsGrad ? distill_launch<kDsGrad>(p, type, cluster, smem, s) : distill_launch<kDsStep>(p, type, cluster, smem, s));
+    return SLIM_OK;
+}
+
+}  // namespace slim
+
+extern "C" int slim_distill_loss(const void* logits, int type, long long ld, const void* index, int index_bytes, const void* value, int value_type,
+                                 const float* teacher_lse, double temperature, int M, int V, int k, float* loss, float* saved, void* stream) {
+    return slim::distill(slim::kDsLoss, logits, type, ld, index, index_bytes, value, value_type, teacher_lse, temperature, M, V, k, loss, saved,
+                         nullptr, nullptr, 0, stream);
+}
+extern "C" int slim_distill_grad(const void* logits, int type, long long ld, const void* index, int index_bytes, const void* value, int value_type,
+                                 const float* teacher_lse, double temperature, int M, int V, int k, const float* saved, const float* dloss, void* grad,
+                                 long long ldg, void* stream) {
+    return slim::distill(slim::kDsGrad, logits, type, ld, index, index_bytes, value, value_type, teacher_lse, temperature, M, V, k, nullptr,
+                         const_cast<float*>(saved), dloss, grad, ldg, stream);
+}
+extern "C" int slim_distill_step(const void* logits, int type, long long ld, const void* index, int index_bytes, const void* value, int value_type,
+                                 const float* teacher_lse, double temperature, int M, int V, int k, const float* dloss, float* loss, void* grad,
+                                 long long ldg, void* stream) {
+    return slim::distill(slim::kDsStep, logits, type, ld, index, index_bytes, value, value_type, teacher_lse, temperature, M, V, k, loss, nullptr,
+                         dloss, grad, ldg, stream);
+}

@@ -212,3 +212,21 @@ def test_large_layers_ask_for_room_for_their_cut_row_blocks_alone(slim, N, K, M,
     parts = 148 + min(148, (N + rows - 1) // rows)
     staged = K // 128 * mv * (3 * 128 + 8)
     assert slim.workspace_bytes(M, N, K, np.full(K // 128, b, np.uint8)) <= 2048 + 1024 + 256 + parts * M * rows * 4 + staged
+
+
+def test_distillation_argument_errors(slim):
+    """Everything that is refused is refused before a pointer is read: the addresses here are not memory."""
+    L = slim.lib()
+    a = 1 << 20                                                                              # "device" addresses, 16-byte aligned
+    loss = lambda ld=100, type_=1, ib=8, vt=0, T=1.0, M=2, V=100, k=4, out=a, logits=a, index=a, saved=a: L.slim_distill_loss(
+        logits, type_, ld, index, ib, a, vt, None, ctypes.c_double(T), M, V, k, out, saved, None)
+    assert loss(M=0) == 0
+    assert loss(M=-1) == -1 and loss(V=0) == -1 and loss(k=0) == -1 and loss(ld=99) == -1
+    assert loss(type_=3) == -1 and loss(vt=-1) == -1 and loss(ib=2) == -1
+    assert loss(T=0.0) == -1 and loss(T=-2.0) == -1 and loss(T=float("nan")) == -1 and loss(T=float("inf")) == -1
+    assert loss(out=None) == -1 and loss(logits=None) == -1 and loss(index=None) == -1
+    assert loss(k=1025) == -2 and loss(V=2097153, ld=2097153) == -2
+    assert loss(logits=a + 1) == -3 and loss(index=a + 4) == -3 and loss(saved=a + 4) == -3
+    step = lambda ldg=100, dloss=a, grad=a: L.slim_distill_step(a, 1, 100, a, 8, a, 0, None, ctypes.c_double(1.0), 2, 100, 4, dloss, a, grad, ldg, None)
+    assert step(ldg=99) == -1 and step(dloss=None) == -1 and step(grad=None) == -1 and step(grad=a + 1) == -3
+    assert L.slim_distill_grad(a, 1, 100, a, 8, a, 0, None, ctypes.c_double(1.0), 2, 100, 4, None, a, a, 100, None) == -1      # nothing saved
