@@ -80,6 +80,9 @@ def lib():
             "slim_gptq_workspace_bytes": [i, i, i, i, ctypes.POINTER(sz)],
             "slim_gptq_factor": [vp, i, i, ctypes.c_double, vp, vp, vp, sz, vp],
             "slim_gptq_quantize": [vp, vp, vp, ctypes.c_double, i, vp, vp, vp, vp, i, i, i, i, vp, sz, vp],
+            "slim_fp8_quantize": [vp, i, ll, vp, vp, i, i, vp],
+            "slim_fp8_workspace_bytes": [i, i, i, ctypes.POINTER(sz)],
+            "slim_fp8_linear": [vp, i, ll, vp, vp, vp, i, ll, i, i, i, vp, sz, vp],
             "slim_distill_loss": [vp, i, ll, vp, i, vp, i, vp, ctypes.c_double, i, i, i, vp, vp, vp],
             "slim_distill_grad": [vp, i, ll, vp, i, vp, i, vp, ctypes.c_double, i, i, i, vp, vp, vp, ll, vp],
             "slim_distill_step": [vp, i, ll, vp, i, vp, i, vp, ctypes.c_double, i, i, i, vp, vp, vp, ll, vp],
@@ -383,6 +386,51 @@ class _device_of:
             torch.cuda.set_device(self.back)
 
 
+def fp8_quantize(W: torch.Tensor):
+    """W (fp32, fp16 or bf16 [N][K], K a multiple of 16, rows may be strided) in e4m3 with a power-of-two scale per block
+    of 128 x 128 (slim_fp8_quantize).  Returns codes (float8_e4m3fn [N][K]) and scales (fp32 [ceil(N/128)][ceil(K/128)])."""
+    ld = _rows(W, "W", _TYPES)
+    N, K = W.shape
+    codes = torch.empty((N, K), dtype=torch.float8_e4m3fn, device=W.device)
+    scales = torch.empty(((N + 127) // 128, (K + 127) // 128), dtype=torch.float32, device=W.device)
+    with _device_of(W):
+        _check("slim_fp8_quantize", lib().slim_fp8_quantize(W.data_ptr(), _TYPES[W.dtype], ld, codes.data_ptr(), scales.data_ptr(), N, K, _stream(W)))
+    return codes, scales
+
+
+def fp8_workspace_bytes(M: int, N: int, K: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("slim_fp8_workspace_bytes", lib().slim_fp8_workspace_bytes(M, N, K, ctypes.byref(out)))
+    return out.value
+
+
+def fp8_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor | None = None,
+               out_dtype: torch.dtype | None = None) -> torch.Tensor:
+    """y = x W^T with W in e4m3 under a scale per block of 128 x 128, x (fp16 or bf16 [M][K], rows may be strided) quantised
+    inside the call (slim_fp8_linear).  y is of x's type, or fp32 (out_dtype, or out's)."""
+    ldx = _rows(x, "x", (torch.float16, torch.bfloat16))
+    M, K = x.shape
+    cp, sp, wp = _dev(codes, torch.float8_e4m3fn, "codes"), _dev(scales, torch.float32, "scales"), _dev(workspace, torch.uint8, "workspace")
+    if codes.dim() != 2 or codes.shape[1] != K:
+        raise ValueError(f"codes must be [N][{K}]")
+    N = codes.shape[0]
+    if tuple(scales.shape) != ((N + 127) // 128, (K + 127) // 128):
+        raise ValueError(f"scales must be [{(N + 127) // 128}][{(K + 127) // 128}]")
+    if not (codes.device == scales.device == workspace.device == x.device):
+        raise ValueError(f"codes, scales and workspace must be on {x.device}")
+    if out is None:
+        out = torch.empty((M, N), dtype=x.dtype if out_dtype is None else out_dtype, device=x.device)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise ValueError(f"out is not of dtype {out_dtype}")
+    ldy = _rows(out, "out", (x.dtype, torch.float32), x.device)
+    if tuple(out.shape) != (M, N):
+        raise ValueError(f"out must be [{M}][{N}]")
+    with _device_of(x):
+        _check("slim_fp8_linear", lib().slim_fp8_linear(x.data_ptr(), _TYPES[x.dtype], ldx, cp, sp, out.data_ptr(), _TYPES[out.dtype], ldy, M, N, K,
+                                                        wp, workspace.numel(), _stream(x)))
+    return out
+
+
 def _distill_args(logits, top_index, top_logit, temperature, teacher_lse):
     ld = _rows(logits, "logits", _TYPES)
     M, V = logits.shape
@@ -621,3 +669,47 @@ class QuantLinear:
     def algorithmic_bytes(self, M: int) -> int:
         G = self.K // self.g
         return self.packed.numel() + 2 * 2 * G * self.N + G + 2 * M * self.K + 2 * M * self.N
+
+
+class Fp8Linear:
+    """One layer in 8-bit floats resident on the device: e4m3 codes [N][K] and a scale per block of 128 x 128.
+
+    The weight is frozen; input_grad is the gradient of the layer's input, the same product with the transposed codes, which
+    prepare_input_grad lays out once (as many bytes again; N a multiple of 16)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        _dev(codes, torch.float8_e4m3fn, "codes"), _dev(scales, torch.float32, "scales")
+        if codes.dim() != 2 or tuple(scales.shape) != ((codes.shape[0] + 127) // 128, (codes.shape[1] + 127) // 128):
+            raise ValueError("codes must be [N][K] and scales [ceil(N/128)][ceil(K/128)]")
+        self.codes, self.scales = codes, scales
+        self.N, self.K = codes.shape
+        self._codes_t = self._scales_t = None
+
+    @classmethod
+    def from_weight(cls, W: torch.Tensor) -> "Fp8Linear":
+        return cls(*fp8_quantize(W))
+
+    def new_workspace(self, M: int, input_grad: bool = False) -> torch.Tensor:
+        """A workspace, initialised, for forward (or input_grad) with up to M tokens."""
+        n = fp8_workspace_bytes(M, self.K, self.N) if input_grad else fp8_workspace_bytes(M, self.N, self.K)
+        ws = torch.empty(n, dtype=torch.uint8, device=self.codes.device)
+        with _device_of(ws):
+            workspace_init(ws)
+        return ws
+
+    def forward(self, x: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None) -> torch.Tensor:
+        return fp8_linear(x, self.codes, self.scales, workspace, out, out_dtype)
+
+    def prepare_input_grad(self) -> None:
+        """Lays the transposed codes and scales out, unless they are there already."""
+        if self._codes_t is None:
+            if self.N % 16:
+                raise ValueError("the gradient of the input needs a number of output features that is a multiple of 16")
+            self._codes_t = self.codes.view(torch.uint8).t().contiguous().view(torch.float8_e4m3fn)
+            self._scales_t = self.scales.t().contiguous()
+
+    def input_grad(self, dy: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor | None = None,
+                   out_dtype: torch.dtype | None = None) -> torch.Tensor:
+        """dx = dy W for dy [M][N], quantised in the call like forward's x."""
+        self.prepare_input_grad()
+        return fp8_linear(dy, self._codes_t, self._scales_t, workspace, out, out_dtype)

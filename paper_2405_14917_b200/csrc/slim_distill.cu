@@ -98,6 +98,46 @@ template <> struct DsType<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 round(float v) { return __float2bfloat16_rn(v); }
 };
 
+// Largest of a thread's vectors, two elements at a time where they are 16 bits wide (a NaN loses: it shows in the sum).
+__device__ __forceinline__ float vec_max(const uint4* x, int n, const float*) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kDsVecs; ++u)
+        m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(x[u].x), __uint_as_float(x[u].y)), fmaxf(__uint_as_float(x[u].z), __uint_as_float(x[u].w))));
+    return m;
+}
+template <typename H2, typename T>
+__device__ __forceinline__ float vec_max2(const uint4* x, T) {
+    auto h = [](const uint32_t& w) { return *reinterpret_cast<const H2*>(&w); };
+    H2 m = h(x[0].x);
+#pragma unroll
+    for (int u = 0; u < kDsVecs; ++u) m = __hmax2(m, __hmax2(__hmax2(h(x[u].x), h(x[u].y)), __hmax2(h(x[u].z), h(x[u].w))));
+    const float a = DsType<T>::one(m.x), b = DsType<T>::one(m.y);
+    return fmaxf(fmaxf(a, b), -INFINITY);
+}
+__device__ __forceinline__ float vec_max(const uint4* x, int, const __half*) { return vec_max2<__half2>(x, __half()); }
+__device__ __forceinline__ float vec_max(const uint4* x, int, const __nv_bfloat16*) { return vec_max2<__nv_bfloat162>(x, __nv_bfloat16()); }
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// The vectors again, as values that the compiler takes for new: it would otherwise keep all of them unpacked from one pass to the next.
+__device__ __forceinline__ void forget(uint4& v) { asm volatile("" : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w)); }
+
 __device__ __forceinline__ float ex2(float v) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -145,20 +185,22 @@ struct Slice {
     }
 };
 
+// Shared memory of k entries (a multiple of 16 bytes).
+__host__ __device__ __forceinline__ int entry_bytes(int k) { return (25 * k + 16 + 15) & ~15; }
+
 template <typename T, bool REST, int MODE>
 __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillParams p) {
     constexpr int E = DsType<T>::E;
     extern __shared__ __align__(16) unsigned char ds_smem[];
     double* s_q = reinterpret_cast<double*>(ds_smem);                  // [k] teacher's probability
     double* s_lq = s_q + p.k;                                          // [k] its logarithm
-    int* s_idx = reinterpret_cast<int*>(s_lq + p.k);                   // [k] column, -1 where the entry is absent
-    float* s_s = reinterpret_cast<float*>(s_idx + p.k);                // [k] student's logit
+    int* s_idx = reinterpret_cast<int*>(s_lq + p.k);                   // [k + 4] column, -1 where the entry is absent
+    float* s_s = reinterpret_cast<float*>(s_idx + p.k + 4);            // [k] student's logit
     uint8_t* s_first = reinterpret_cast<uint8_t*>(s_s + p.k);          // [k] no entry before it has this column
-    uint32_t* s_mark = reinterpret_cast<uint32_t*>(ds_smem + ((25 * p.k + 15) & ~15));    // REST: bit e of byte j: element e of vector j is listed
-    __shared__ float s_max[kDsWarps];
-    __shared__ double s_sum[kDsWarps];
+    uint32_t* s_mark = reinterpret_cast<uint32_t*>(ds_smem + entry_bytes(p.k));    // REST: bit e of byte j: element e of vector j is listed
+    __shared__ float2 s_part[kDsWarps];                                // maximum and sum of every warp's columns
     __shared__ float2 s_slice;                                         // maximum and sum of this slice, for the cluster
-    __shared__ double s_row[8];
+    __shared__ double s_row[2];                                         // the teacher's listed mass; whether there is any
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ranks = p.ranks;
@@ -171,7 +213,8 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
 #pragma unroll
     for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(tid + u * kDsThreads);
 
-    // ---- the entries: columns, the teacher's values, the student's logits at them
+    // ---- the entries: columns, the teacher's values, the student's logits at them (wanted last, and fetched meanwhile)
+    float early = 0.f;
     for (int j = tid; j < p.k; j += kDsThreads) {
         const size_t at = static_cast<size_t>(row) * p.k + j;
         const long long i = p.index64 ? static_cast<const long long*>(p.index)[at] : static_cast<const int*>(p.index)[at];
@@ -181,35 +224,42 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
         else if (p.value_type == SLIM_F16) u = __half2float(static_cast<const __half*>(p.value)[at]);
         else u = __bfloat162float(static_cast<const __nv_bfloat16*>(p.value)[at]);
         s_idx[j] = in ? static_cast<int>(i) : -1;
-        s_s[j] = in ? DsType<T>::one(r_logits[i]) : 0.f;
+        const float sv = in ? DsType<T>::one(r_logits[i]) : 0.f;
+        if (j == tid) early = sv;
+        else s_s[j] = sv;
         s_lq[j] = u * p.inv_t;
     }
+    if (tid < 4) s_idx[p.k + tid] = -1;              // the search below reads whole quadruples
     if (REST)
         for (int j = tid; j < p.mark_bytes / 4; j += kDsThreads) s_mark[j] = 0u;
     __syncthreads();
+    int twice = 0;                                   // an entry of this thread has the column of one before it
     for (int j = tid; j < p.k; j += kDsThreads) {
         const int i = s_idx[j];
-        bool first = i >= 0;
-        for (int o = 0; o < j; ++o) first = first && s_idx[o] != i;
-        s_first[j] = first;
+        bool again = false;
+        for (int o = 0; o < j; o += 4) {
+            const int4 c = *reinterpret_cast<const int4*>(s_idx + o);
+            again = again || (c.x == i) || (o + 1 < j && c.y == i) || (o + 2 < j && c.z == i) || (o + 3 < j && c.w == i);
+        }
+        s_first[j] = i >= 0 && !again;
+        twice |= i >= 0 && again;
         if (REST && i >= v0 && i < v1) {
             const int e = i - v0 + sl.shift;
             atomicOr(s_mark + (e / E >> 2), 1u << ((e / E & 3) * 8 + e % E));
         }
     }
-    if (warp == 0) {
+    if (warp == kDsWarps - 1) {
         // the teacher's probabilities; a row has something to learn from if an entry is present (and, without the rest, not all of them are minus infinity)
         double top = -INFINITY;
         int any = 0, finite = 0;
         for (int j = lane; j < p.k; j += 32)
             if (s_idx[j] >= 0) { top = fmax(top, s_lq[j]); any = 1; finite |= !(s_lq[j] == -INFINITY); }
         any = __any_sync(0xffffffffu, any);
-        finite = __any_sync(0xffffffffu, finite);
         double norm;
         if (REST) norm = p.lse[row];
         else {
+            any = __any_sync(0xffffffffu, finite);
             top = warp_max(top);
-            any = finite;
             double sum = 0.0;
             for (int j = lane; j < p.k; j += 32)
                 if (s_idx[j] >= 0) sum += exp(s_lq[j] - top);
@@ -226,12 +276,13 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
         q_sum = warp_sum(q_sum);
         if (lane == 0) { s_row[0] = q_sum; s_row[1] = any; }
     }
-    __syncthreads();
+    twice = __syncthreads_or(twice);
 
     // ---- the row's maximum and sum of exponentials, of the columns outside the set with REST
     float m;
     double R;                                        // sum over the columns (outside the set) of 2^((s - m) c)
     const uint8_t* mark = reinterpret_cast<const uint8_t*>(s_mark);
+    const uint64_t c2 = pair2(p.c, p.c);
     if (MODE != kDsGrad) {
         float tm = -INFINITY, ts = 0.f;
         for (int j0 = 0; j0 < sl.nv; j0 += kDsVecs * kDsThreads) {
@@ -239,172 +290,177 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
 #pragma unroll
                 for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(j0 + tid + u * kDsThreads);
             }
-            float cm = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < kDsVecs; ++u) {
-                float f[E];
-                DsType<T>::unpack(x[u], f);
-#pragma unroll
-                for (int e = 0; e < E; ++e) cm = fmaxf(cm, f[e]);
-            }
+            const float cm = vec_max(x, kDsVecs, static_cast<const T*>(nullptr));
             if (cm > tm) { ts *= tm == -INFINITY ? 0.f : ex2((tm - cm) * p.c); tm = cm; }
-            const float ref = tm == -INFINITY ? 0.f : tm;
+            const float neg = tm == -INFINITY ? 0.f : -tm;
+            const uint64_t neg2 = pair2(neg, neg);
+            uint64_t acc = pair2(ts, 0.f);
 #pragma unroll
             for (int u = 0; u < kDsVecs; ++u) {
-                float f[E];
-                DsType<T>::unpack(x[u], f);
+                forget(x[u]);
                 const int j = j0 + tid + u * kDsThreads;
-                if (REST && j < sl.nv) {
-                    const uint32_t b = mark[j];
-                    if (b != 0) {
+                if (j < sl.nv) {
+                    float f[E];
+                    DsType<T>::unpack(x[u], f);
+                    if (REST) {
+                        const uint32_t b = mark[j];
+                        if (b != 0) {
 #pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            if (b >> e & 1u) f[e] = -INFINITY;
+                            for (int e = 0; e < E; ++e)
+                                if (b >> e & 1u) f[e] = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < E; e += 2) {
+                        float a, b;
+                        unpair2(mul2(add2(pair2(f[e], f[e + 1]), neg2), c2), a, b);
+                        acc = add2(acc, pair2(ex2(a), ex2(b)));
                     }
                 }
-                float s = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) s += ex2((f[e] - ref) * p.c);
-                ts += s;
             }
+            float a, b;
+            unpair2(acc, a, b);
+            ts = a + b;
         }
+        // a warp's, then the slice's, then the row's
         float wm = tm;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor_sync(0xffffffffu, wm, o));
-        if (lane == 0) s_max[warp] = wm;
-        __syncthreads();
-        m = s_max[0];
+        float ws = tm == -INFINITY ? ts : ts * ex2((tm - wm) * p.c);
 #pragma unroll
-        for (int w = 1; w < kDsWarps; ++w) m = fmaxf(m, s_max[w]);
-        const double ws = warp_sum(tm == -INFINITY ? static_cast<double>(ts) : static_cast<double>(ts * ex2((tm - m) * p.c)));
-        if (lane == 0) s_sum[warp] = ws;
+        for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
+        if (lane == 0) s_part[warp] = make_float2(wm, ws);
+        if (tid < p.k) s_s[tid] = early;
         __syncthreads();
-        R = 0.0;
+        auto join = [&](float2 part, bool in) {
+            m = in ? part.x : -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kDsWarps; ++w) R += s_sum[w];
+            for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            R = warp_sum(!in ? 0.0 : part.x == -INFINITY ? static_cast<double>(part.y) : static_cast<double>(part.y) * static_cast<double>(ex2((part.x - m) * p.c)));
+        };
+        join(s_part[lane % kDsWarps], lane < kDsWarps);
         if (ranks > 1) {
             if (tid == 0) s_slice = make_float2(m, static_cast<float>(R));
             cluster_sync_all();
-            const uint32_t at = smem_u32(&s_slice);
-            float mm = -INFINITY;
-            for (int r = 0; r < ranks; ++r) mm = fmaxf(mm, ld_cluster_f32x2(at, r).x);
-            R = 0.0;
-            for (int r = 0; r < ranks; ++r) {
-                const float2 o = ld_cluster_f32x2(at, r);
-                R += o.x == -INFINITY ? static_cast<double>(o.y) : static_cast<double>(o.y) * static_cast<double>(ex2((o.x - mm) * p.c));
-            }
-            m = mm;
+            join(ld_cluster_f32x2(smem_u32(&s_slice), lane % ranks), lane < ranks);
         }
     } else {
         const float4 sv = *reinterpret_cast<const float4*>(p.saved + 4 * static_cast<size_t>(row));
         m = sv.x;
         R = REST ? sv.z : sv.y;
+        if (tid < p.k) s_s[tid] = early;
+        __syncthreads();
         if (ranks > 1) cluster_sync_all();           // grad may be logits: every CTA of the row has its entries' logits
     }
 
-    // ---- what the row comes to: by warp 0, in 64 bits
-    if (warp == 0) {
-        const double ln2 = 0.69314718055994530942, cd = p.c, md = m == -INFINITY ? 0.0 : static_cast<double>(m);
-        double Z = R;
-        if (REST) {
-            double z = 0.0;
-            for (int j = lane; j < p.k; j += 32)
-                if (s_first[j]) z += exp((static_cast<double>(s_s[j]) - md) * cd * ln2);
-            Z += warp_sum(z);
-        }
-        if (MODE == kDsGrad) Z = p.saved[4 * static_cast<size_t>(row) + 1];
-        const double lz = log(Z), q_sum = s_row[0];
-        const bool any = s_row[1] != 0.0;
-        double l = 0.0, p_in = 0.0;
+    // ---- what the row comes to, by every warp for itself: Z, and the masses of the set and of the rest
+    const float ref = m == -INFINITY ? 0.f : m;
+    const double q_sum = s_row[0];
+    const bool any = s_row[1] != 0.0;
+    double Z = R, p_rest = 0.0, q_rest = 0.0, p_in = 0.0;
+    bool little = false;                             // the set has less than half of the mass: the rest is what it leaves of 1
+    if (REST) {
+        double z = 0.0;
         int columns = 0;
+        for (int j = lane; j < p.k; j += 32)
+            if (s_first[j]) { z += ex2((s_s[j] - ref) * p.c); ++columns; }
+        z = warp_sum(z);
+        Z += z;
+        p_in = Z == 0.0 ? 0.0 : z / Z;
+        little = p_in < 0.5;
+        p_rest = Z == 0.0 ? 0.0 : little ? 1.0 - p_in : R / Z;
+        q_rest = static_cast<int>(__reduce_add_sync(0xffffffffu, columns)) < p.V ? fmax(1.0 - q_sum, 0.0) : 0.0;
+        if (q_sum != q_sum) q_rest = q_sum;          // a NaN among the teacher's values
+    }
+    // loss, in 64 bits, by the warp that is given it (below, beside the gradient)
+    auto write_loss = [&] {
+        const double ln2 = 0.69314718055994530942, cd = p.c, lz = log(Z);
+        double l = 0.0;
         for (int j = lane; j < p.k; j += 32) {
-            if (s_idx[j] < 0) continue;
-            const double lp = Z == 0.0 ? -INFINITY : (static_cast<double>(s_s[j]) - md) * cd * ln2 - lz;
-            if (!(s_q[j] == 0.0)) l += s_q[j] * (s_lq[j] - lp);
-            if (REST && s_first[j]) { p_in += exp(lp); ++columns; }
+            const double q = s_q[j];
+            if (s_idx[j] < 0 || q == 0.0) continue;
+            l += q * (s_lq[j] - (Z == 0.0 ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(ref)) * cd * ln2 - lz));
         }
         l = warp_sum(l);
-        double mass = q_sum, other = q_sum;          // factor of p_v in the gradient of the listed columns, of the others
-        if (REST) {
-            p_in = warp_sum(p_in);
-            // the mass outside the set: what the listed columns leave of 1, unless that would cancel
-            const bool little = p_in < 0.5;
-            const double p_rest = Z == 0.0 ? 0.0 : little ? 1.0 - p_in : R / Z;
-            const bool others = __reduce_add_sync(0xffffffffu, columns) < p.V;
-            const double q_rest = others ? fmax(1.0 - q_sum, 0.0) : 0.0;
-            mass = q_sum + q_rest;
-            other = mass;
-            if (q_rest > 0.0) {
-                l += q_rest * (log(q_rest) - (p_rest == 0.0 ? -INFINITY : little ? log1p(-p_in) : log(p_rest)));
-                other = p_rest == 0.0 ? 0.0 : mass - q_rest / p_rest;
-            }
-            if (q_sum != q_sum) mass = other = l = q_sum;          // a NaN among the teacher's values
-        }
+        if (REST && !(q_rest == 0.0)) l += q_rest * (log(q_rest) - (p_rest == 0.0 ? -INFINITY : little ? log1p(-p_in) : log(p_rest)));
         if (lane == 0) {
-            if (MODE != kDsGrad && rank == 0) {
-                p.loss[row] = any ? static_cast<float>(l) : 0.f;
-                if (MODE == kDsLoss && p.saved != nullptr)
-                    *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) =
-                        make_float4(m, static_cast<float>(Z), static_cast<float>(R), 0.f);
-            }
-            if (MODE != kDsLoss) {
-                const double d = static_cast<double>(p.dloss[row]) * p.inv_t;
-                s_row[2] = mass * d;
-                s_row[3] = Z == 0.0 ? 0.0 : other * d / Z;
-                s_row[4] = Z == 0.0 ? 0.0 : 1.0 / Z;
-                s_row[5] = d;
-            }
+            p.loss[row] = any ? static_cast<float>(l) : 0.f;
+            if (MODE == kDsLoss && p.saved != nullptr)
+                *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) = make_float4(m, static_cast<float>(Z), static_cast<float>(R), 0.f);
         }
-    }
+    };
     if (MODE == kDsLoss) {
+        if (rank == 0 && warp == 0) write_loss();
         if (ranks > 1) cluster_sync_all();           // the others may still read this CTA's slice statistics
         return;
     }
-    __syncthreads();
 
     // ---- the gradient: one factor for the whole row, then the listed columns
-    const bool any = s_row[1] != 0.0;
-    const float ref = m == -INFINITY ? 0.f : m;
-    const float factor = any ? static_cast<float>(s_row[3]) : 0.f;
+    // Without a mass outside, or for the listed columns, p_v is multiplied by the teacher's whole mass; with one, that of the others is
+    // 1 - q'/p' = (p' - q') / p', and p' - q' = sum q - p_in where p' is what p_in leaves of 1.
+    const double d = static_cast<double>(p.dloss[row]) * p.inv_t;
+    const float inv_z = Z == 0.0 ? 0.f : 1.f / static_cast<float>(Z);
+    const double mass = q_sum + q_rest;
+    float other = static_cast<float>(mass);
+    if (REST && !(q_rest == 0.0))
+        other = p_rest == 0.0 ? 0.f : static_cast<float>(little ? q_sum - p_in : p_rest - q_rest) / static_cast<float>(p_rest);
+    const float factor = any ? other * inv_z * static_cast<float>(d) : 0.f;
     T* r_grad = static_cast<T*>(p.grad) + static_cast<long long>(row) * p.ldg;
     T* g_base = r_grad + v0 - sl.shift;
     const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
+    const uint64_t neg2 = pair2(-ref, -ref), factor2 = pair2(factor, factor);
     for (int j0 = 0; j0 < sl.nv; j0 += kDsVecs * kDsThreads) {
-        if (sl.nv > kDsVecs * kDsThreads) {          // more than the registers hold: read again
+        if (MODE == kDsStep && sl.nv > kDsVecs * kDsThreads) {          // more than the registers hold: read again
+#pragma unroll
+            for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(j0 + tid + u * kDsThreads);
+        }
+        if (MODE == kDsGrad && j0 > 0) {
 #pragma unroll
             for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(j0 + tid + u * kDsThreads);
         }
 #pragma unroll
         for (int u = 0; u < kDsVecs; ++u) {
+            forget(x[u]);
             const int j = j0 + tid + u * kDsThreads;
-            if (j >= sl.nv) break;
-            float f[E];
-            DsType<T>::unpack(x[u], f);
+            if (j < sl.nv) {
+                float f[E];
+                DsType<T>::unpack(x[u], f);
 #pragma unroll
-            for (int e = 0; e < E; ++e) f[e] = any ? ex2((f[e] - ref) * p.c) * factor : 0.f;
-            if (vectors && sl.whole(j)) __stcs(reinterpret_cast<uint4*>(g_base) + j, DsType<T>::pack(f));
-            else {
+                for (int e = 0; e < E; e += 2) {
+                    float a, b;
+                    unpair2(mul2(add2(pair2(f[e], f[e + 1]), neg2), c2), a, b);
+                    unpair2(mul2(pair2(ex2(a), ex2(b)), factor2), f[e], f[e + 1]);
+                }
+                if (!any) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int i = j * E + e;
-                    if (i >= sl.shift && i < sl.end) g_base[i] = DsType<T>::round(f[e]);
+                    for (int e = 0; e < E; ++e) f[e] = 0.f;
+                }
+                if (vectors && sl.whole(j)) __stcs(reinterpret_cast<uint4*>(g_base) + j, DsType<T>::pack(f));
+                else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const int i = j * E + e;
+                        if (i >= sl.shift && i < sl.end) g_base[i] = DsType<T>::round(f[e]);
+                    }
                 }
             }
         }
     }
     __syncthreads();                                 // the listed columns are written over
     if (any) {
-        const double ln2 = 0.69314718055994530942, cd = p.c, md = m == -INFINITY ? 0.0 : static_cast<double>(m);
         for (int j = tid; j < p.k; j += kDsThreads) {
             const int i = s_idx[j];
             if (!s_first[j] || i < v0 || i >= v1) continue;
-            double q = 0.0;
-            for (int o = j; o < p.k; ++o) q += s_idx[o] == i ? s_q[o] : 0.0;
-            const double e = exp((static_cast<double>(s_s[j]) - md) * cd * ln2);
-            r_grad[i] = DsType<T>::round(static_cast<float>(e * s_row[4] * s_row[2] - q * s_row[5]));
+            double q = s_q[j];
+            if (twice)
+                for (int o = j + 1; o < p.k; ++o) q += s_idx[o] == i ? s_q[o] : 0.0;
+            r_grad[i] = DsType<T>::round(static_cast<float>((static_cast<double>(ex2((s_s[j] - ref) * p.c) * inv_z) * mass - q) * d));
         }
     }
-    if (MODE == kDsStep && ranks > 1) cluster_sync_all();
+    if (MODE == kDsStep) {
+        if (rank == 0 && warp == kDsWarps - 1) write_loss();
+        if (ranks > 1) cluster_sync_all();
+    }
 }
 
 // ------------------------------------------------------------------------------------------ host side
@@ -482,7 +538,7 @@ static int distill(int mode, const void* logits, int type, long long ld, const v
     p.ranks = cluster;
     p.slice = ((V + cluster - 1) / cluster + E - 1) / E * E;
     p.mark_bytes = lse != nullptr ? (p.slice / E + 1 + 3) / 4 * 4 : 0;
-    const size_t smem = ((25 * static_cast<size_t>(k) + 15) & ~static_cast<size_t>(15)) + p.mark_bytes;
+    const size_t smem = static_cast<size_t>(entry_bytes(k)) + p.mark_bytes;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     SLIM_CUDA_TRY(mode == kDsLoss ? distill_launch<kDsLoss>(p, type, cluster, smem, s)
                   : mode == kDsGrad ? distill_launch<kDsGrad>(p, type, cluster, smem, s) : distill_launch<kDsStep>(p, type, cluster, smem, s));

@@ -1,0 +1,188 @@
+// slim_fp8_quantize, slim_fp8_linear: a linear layer in 8-bit floats (e4m3), the group-wise layer's counterpart for the weights that
+// one to four bits do not do: W in blocks of 128 x 128 with one fp32 scale each, x quantised inside the call in blocks of 128 columns of a token,
+//     y[m][n] = sum_g sx[m][g] * sw[n / 128][g] * sum_{k in block g} xq[m][k] * wq[n][k]
+// with the inner sums on the tensor cores (tcgen05, e4m3 in, fp32 accumulator) and the outer one in fp32 registers.
+// This file: the two quantizers, which kernel a call goes to, and the entry points.
+#include "slim_fp8.cuh"
+
+#include <atomic>
+
+namespace slim {
+
+// ------------------------------------------------------------------------------------------ W
+// A block of 256 threads per 128 x 128 block of W; thread (r, c): row r + 16 i, columns 8c .. 8c + 7.  Bound: HBM, one read and
+// one write; the block stays in registers between its maximum and its codes.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float* f) { f8::unpack8<T>(__ldcs(reinterpret_cast<const uint4*>(p)), f); }
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float* f) {
+    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+template <typename T>
+__global__ void __launch_bounds__(256) fp8_quantize_kernel(const T* __restrict__ W, long long ld, uint8_t* __restrict__ codes,
+                                                           float* __restrict__ scales, int N, int K) {
+    __shared__ uint32_t s_max[8];
+    const int tid = threadIdx.x, c = tid & 15, r = tid >> 4;
+    const int n0 = blockIdx.y * f8::kBlock, k = blockIdx.x * f8::kBlock + 8 * c;
+    float f[8][8];
+    uint32_t mx = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int n = n0 + r + 16 * i;
+        if (n < N && k < K) load8(W + static_cast<size_t>(n) * ld + k, f[i]);
+        else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[i][e] = 0.f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mx = max(mx, f8::magnitude(f[i][e]));
+    mx = __reduce_max_sync(0xffffffffu, mx);
+    if ((tid & 31) == 0) s_max[tid >> 5] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) mx = max(mx, s_max[w]);
+    const uint32_t sb = f8::scale_bits(mx);
+    const float inv = f8::inverse_scale(sb);
+    if (tid == 0) scales[static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x] = __uint_as_float(sb);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int n = n0 + r + 16 * i;
+        if (n < N && k < K)
+            *reinterpret_cast<uint2*>(codes + static_cast<size_t>(n) * K + k) = make_uint2(f8::codes4(f[i], inv), f8::codes4(f[i] + 4, inv));
+    }
+}
+
+// ------------------------------------------------------------------------------------------ x
+// Half a warp per block of 128 columns of a token, 8 columns per lane.  The kernel that reads the codes may be set up meanwhile.
+template <typename T>
+__global__ void __launch_bounds__(256) fp8_stage_kernel(const T* __restrict__ x, long long ld, uint8_t* __restrict__ codes,
+                                                        float* __restrict__ scales, int M, int K, int G, int Mp) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const long long unit = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) >> 4;
+    const int c = threadIdx.x & 15;
+    const int m = static_cast<int>(unit / G), g = static_cast<int>(unit - static_cast<long long>(m) * G);
+    const int k = g * f8::kBlock + 8 * c;
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = 0.f;
+    const bool in = m < M && k < K;
+    if (in) f8::unpack8<T>(*reinterpret_cast<const uint4*>(x + static_cast<size_t>(m) * ld + k), f);
+    uint32_t mx = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mx = max(mx, f8::magnitude(f[e]));
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const uint32_t sb = f8::scale_bits(mx);
+    const float inv = f8::inverse_scale(sb);
+    if (in) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(m) * K + k) = make_uint2(f8::codes4(f, inv), f8::codes4(f + 4, inv));
+    if (c == 0 && m < M) scales[static_cast<size_t>(g) * Mp + m] = __uint_as_float(sb);
+}
+
+static cudaError_t fp8_stage(const Fp8Args& a, uint8_t* codes, float* scales, int Mp) {
+    const int G = (a.K + f8::kBlock - 1) / f8::kBlock;
+    const long long units = static_cast<long long>(a.M) * G;
+    PdlLaunch l(static_cast<unsigned>((units + 15) / 16), 256, 0, a.stream);
+    if (a.x_type == SLIM_F16)
+        return cudaLaunchKernelEx(&l.cfg, fp8_stage_kernel<__half>, static_cast<const __half*>(a.x), a.ldx, codes, scales, a.M, a.K, G, Mp);
+    return cudaLaunchKernelEx(&l.cfg, fp8_stage_kernel<__nv_bfloat16>, static_cast<const __nv_bfloat16*>(a.x), a.ldx, codes, scales, a.M, a.K, G, Mp);
+}
+
+// ------------------------------------------------------------------------------------------ tensor maps
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool make_byte_map(CUtensorMap* map, const void* p, int rows, int cols, int box_rows) {
+    static std::atomic<EncodeTiledFn> found{nullptr};
+    EncodeTiledFn enc = found.load();
+    if (enc == nullptr) {
+        void* sym = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess) return false;
+        enc = reinterpret_cast<EncodeTiledFn>(sym);
+        found.store(enc);
+    }
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols)};
+    const cuuint32_t box[2] = {128u, static_cast<cuuint32_t>(box_rows)};
+    const cuuint32_t estr[2] = {1u, 1u};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static int fp8_shape(int M, int N, int K) {
+    if (M < 0 || N < 0 || K < 0) return SLIM_ERR_INVALID_ARG;
+    if (K % 16 != 0 || K > SLIM_FP8_MAX_K || M > SLIM_FP8_MAX_M || N > SLIM_FP8_MAX_N) return SLIM_ERR_UNSUPPORTED;
+    return SLIM_OK;
+}
+
+}  // namespace slim
+
+extern "C" int slim_fp8_quantize(const void* W, int type, long long ld, void* codes, float* scales, int N, int K, void* stream) {
+    const int st = slim::fp8_shape(0, N, K);
+    if (st != SLIM_OK) return st;
+    if ((type != SLIM_F32 && type != SLIM_F16 && type != SLIM_BF16) || ld < K) return SLIM_ERR_INVALID_ARG;
+    if (N == 0 || K == 0) return SLIM_OK;
+    if (W == nullptr || codes == nullptr || scales == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (!slim::aligned16(W) || !slim::aligned16(codes) || !slim::aligned16(scales) || ld % (type == SLIM_F32 ? 4 : 8) != 0) return SLIM_ERR_ALIGNMENT;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const dim3 grid((K + 127) / 128, (N + 127) / 128);
+    uint8_t* c = static_cast<uint8_t*>(codes);
+    if (type == SLIM_F32) slim::fp8_quantize_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float*>(W), ld, c, scales, N, K);
+    else if (type == SLIM_F16) slim::fp8_quantize_kernel<__half><<<grid, 256, 0, s>>>(static_cast<const __half*>(W), ld, c, scales, N, K);
+    else slim::fp8_quantize_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(static_cast<const __nv_bfloat16*>(W), ld, c, scales, N, K);
+    SLIM_CUDA_TRY(cudaGetLastError());
+    return SLIM_OK;
+}
+
+extern "C" int slim_fp8_workspace_bytes(int M, int N, int K, size_t* out_bytes) {
+    if (out_bytes == nullptr) return SLIM_ERR_INVALID_ARG;
+    const int st = slim::fp8_shape(M, N, K);
+    if (st != SLIM_OK) return st;
+    *out_bytes = M == 0 || slim::fp8_few_takes_x(M) ? slim::kWsFlagsOffset + slim::kWsFlagsBytes : slim::fp8_staging(M, K).bytes;
+    return SLIM_OK;
+}
+
+extern "C" int slim_fp8_linear(const void* x, int x_type, long long ldx, const void* codes, const float* scales, void* y, int y_type, long long ldy,
+                               int M, int N, int K, void* workspace, size_t workspace_bytes, void* stream) {
+    const int st = slim::fp8_shape(M, N, K);
+    if (st != SLIM_OK) return st;
+    if ((x_type != SLIM_F16 && x_type != SLIM_BF16) || (y_type != x_type && y_type != SLIM_F32) || ldx < K || ldy < N) return SLIM_ERR_INVALID_ARG;
+    if (M == 0 || N == 0) return SLIM_OK;
+    if (y == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (!slim::aligned16(y)) return SLIM_ERR_ALIGNMENT;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (K == 0) {                                      // an empty sum
+        const size_t es = y_type == SLIM_F32 ? 4 : 2;
+        SLIM_CUDA_TRY(cudaMemset2DAsync(y, static_cast<size_t>(ldy) * es, 0, static_cast<size_t>(N) * es, static_cast<size_t>(M), s));
+        return SLIM_OK;
+    }
+    if (x == nullptr || codes == nullptr || scales == nullptr) return SLIM_ERR_INVALID_ARG;
+    if (!slim::aligned16(x) || !slim::aligned16(codes) || !slim::aligned16(scales) || ldx % 8 != 0) return SLIM_ERR_ALIGNMENT;
+    size_t need = 0;
+    slim_fp8_workspace_bytes(M, N, K, &need);
+    if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
+    if (!slim::aligned16(workspace)) return SLIM_ERR_ALIGNMENT;
+    slim::Fp8Args a;
+    memset(&a, 0, sizeof a);
+    a.x = x; a.x_type = x_type; a.ldx = ldx;
+    a.codes = static_cast<const uint8_t*>(codes); a.scales = scales;
+    a.y = y; a.y_type = y_type; a.ldy = ldy;
+    a.M = M; a.N = N; a.K = K;
+    a.workspace = static_cast<uint8_t*>(workspace);
+    a.stream = s;
+    if (!slim::fp8_few_takes_x(M)) {
+        const slim::Fp8Staging sg = slim::fp8_staging(M, K);
+        SLIM_CUDA_TRY(slim::fp8_stage(a, a.workspace + sg.codes, reinterpret_cast<float*>(a.workspace + sg.scales), sg.Mp));
+        a.x_codes = a.workspace + sg.codes;
+        a.x_scales = reinterpret_cast<const float*>(a.workspace + sg.scales);
+        a.Mp = sg.Mp;
+    }
+    SLIM_CUDA_TRY(slim::fp8_use_gemm(M, N, K) ? slim::fp8_gemm(a) : slim::fp8_few(a));
+    return SLIM_OK;
+}

@@ -1,0 +1,151 @@
+// Shared by the kernels of the 8-bit linear layer: the block scale, the codes of 8 elements, element types.
+#pragma once
+
+#include "slim_tc.cuh"
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+
+namespace slim {
+namespace f8 {
+
+constexpr int kBlock = 128;                        // columns, and rows of W, that share a scale
+
+// The smallest power of two s >= amax / 448 (448 = 1.75 * 2^8 is e4m3's largest value), at least 2^-126; 1 for a block of zeros.
+// A power of two, so that v / s is exact and the code's is the only rounding: a block's codes do not depend on how the division is done,
+// and e4m3 being a floating-point type nothing is lost by it but at most one bit of the exponent's range.
+// `amax` as bits of a finite fp32 value >= 0.
+__device__ __forceinline__ uint32_t scale_bits(uint32_t amax) {
+    if (amax == 0) return 127u << 23;
+    if (amax < (1u << 23)) return 1u << 23;        // a subnormal maximum: the scale's lower bound
+    const int e = static_cast<int>(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return static_cast<uint32_t>(max(e, 1)) << 23;
+}
+// 1 / s for s of scale_bits (2^-126 .. 2^119): exact.
+__device__ __forceinline__ float inverse_scale(uint32_t bits) { return __uint_as_float((254u << 23) - bits); }
+
+// Four codes of v * inv; what is not finite becomes NaN (e4m3 has no infinity, and 448 would pass for a value).
+__device__ __forceinline__ uint32_t codes4(const float* v, float inv) {
+    uint16_t lo, hi;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(v[1] * inv), "f"(v[0] * inv));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(v[3] * inv), "f"(v[2] * inv));
+    uint32_t r = static_cast<uint32_t>(lo) | static_cast<uint32_t>(hi) << 16;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (!(fabsf(v[i]) <= 3.402823466e38f)) r |= 0x7fu << (8 * i);
+    return r;
+}
+// Magnitude for the block's maximum: what is not finite does not count.
+__device__ __forceinline__ uint32_t magnitude(float v) {
+    const uint32_t m = __float_as_uint(v) & 0x7fffffffu;
+    return m < 0x7f800000u ? m : 0u;
+}
+
+// Eight elements of a row as floats: 16 bytes of a 16-bit type, 32 of fp32.
+template <typename T> __device__ __forceinline__ void unpack8(const uint4& v, float* f);
+template <> __device__ __forceinline__ void unpack8<__half>(const uint4& v, float* f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        f[2 * i] = t.x; f[2 * i + 1] = t.y;
+    }
+}
+template <> __device__ __forceinline__ void unpack8<__nv_bfloat16>(const uint4& v, float* f) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+
+// y element: `type` is SLIM_F32, SLIM_F16 or SLIM_BF16; one rounding of the fp32 sum.
+__device__ __forceinline__ void store_y(void* y, int type, size_t at, float v) {
+    if (type == SLIM_F32) static_cast<float*>(y)[at] = v;
+    else if (type == SLIM_F16) static_cast<__half*>(y)[at] = __float2half_rn(v);
+    else static_cast<__nv_bfloat16*>(y)[at] = __float2bfloat16_rn(v);
+}
+
+// D[tmem] (+)= A[smem] B[smem]^T, e4m3 in, fp32 accumulate.
+__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Instruction descriptor: e4m3 operands, both K-major, fp32 accumulator, m x n.
+__host__ __device__ constexpr uint32_t idesc(int m, int n) {
+    return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+// 32 lanes x 16 columns of 32 bits
+__device__ __forceinline__ void ld16(uint32_t taddr, uint32_t* v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {      // two fp32 multiply-adds
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t pack2(uint32_t a, uint32_t b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+// Waits, for a millisecond at most and whatever the other roles do, until a barrier's phase completes: what is in flight when a call
+// gives up has landed before its shared memory goes.
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+    const unsigned long long t0 = sb::timer_ns();
+    while (!sb::try_wait(bar, parity) && sb::timer_ns() - t0 < 1000000ull) { }
+}
+
+}  // namespace f8
+
+// Where the quantised activations of a call lie in its workspace: behind the header and the flags of the other calls, which
+// are left alone, the codes [M][K], then the scales [groups][Mp], Mp = M rounded up to 32.
+struct Fp8Staging {
+    size_t codes, scales, bytes;
+    int Mp;
+};
+inline Fp8Staging fp8_staging(int M, int K) {
+    Fp8Staging s;
+    s.Mp = (M + 31) / 32 * 32;
+    s.codes = kWsFlagsOffset + kWsFlagsBytes;
+    s.scales = (s.codes + static_cast<size_t>(M) * K + 255) / 256 * 256;
+    s.bytes = s.scales + static_cast<size_t>((K + f8::kBlock - 1) / f8::kBlock) * s.Mp * sizeof(float);
+    return s;
+}
+
+struct Fp8Args {
+    const void* x;            // [M][K], row stride ldx, or null when staged
+    int x_type;
+    long long ldx;
+    const uint8_t* codes;     // [N][K]
+    const float* scales;      // [ceil(N / 128)][ceil(K / 128)]
+    void* y;
+    int y_type;
+    long long ldy;
+    int M, N, K;
+    uint8_t* workspace;
+    const uint8_t* x_codes;   // staged
+    const float* x_scales;
+    int Mp;
+    cudaStream_t stream;
+};
+
+// Tensor map of a matrix of bytes [rows][cols]: boxes of 128 bytes x `box_rows`, 128-byte swizzle, zeros past the ends.
+bool make_byte_map(CUtensorMap* map, const void* p, int rows, int cols, int box_rows);
+// The kernels for few tokens (slim_fp8_few.cu) and for many (slim_fp8_gemm.cu).
+bool fp8_few_takes_x(int M);                       // quantises x itself
+cudaError_t fp8_few(const Fp8Args& a);
+cudaError_t fp8_gemm(const Fp8Args& a);
+bool fp8_use_gemm(int M, int N, int K);
+
+}  // namespace slim

@@ -230,3 +230,28 @@ def test_distillation_argument_errors(slim):
     step = lambda ldg=100, dloss=a, grad=a: L.slim_distill_step(a, 1, 100, a, 8, a, 0, None, ctypes.c_double(1.0), 2, 100, 4, dloss, a, grad, ldg, None)
     assert step(ldg=99) == -1 and step(dloss=None) == -1 and step(grad=None) == -1 and step(grad=a + 1) == -3
     assert L.slim_distill_grad(a, 1, 100, a, 8, a, 0, None, ctypes.c_double(1.0), 2, 100, 4, None, a, a, 100, None) == -1      # nothing saved
+
+
+def test_8_bit_layer_argument_errors_and_sizes(slim):
+    """Everything that is refused is refused before a pointer is read: the addresses here are not memory."""
+    L = slim.lib()
+    a = 1 << 20
+    out = ctypes.c_size_t(0)
+    assert L.slim_fp8_workspace_bytes(1, 4096, 4096, ctypes.byref(out)) == 0 and out.value == 1280        # header and flags
+    assert L.slim_fp8_workspace_bytes(100, 4096, 400, ctypes.byref(out)) == 0 and out.value >= 1280 + 100 * 400 + 4 * 4 * 100
+    assert L.slim_fp8_workspace_bytes(100, 4096, 400, None) == -1
+    assert L.slim_fp8_workspace_bytes(-1, 16, 16, ctypes.byref(out)) == -1
+    assert L.slim_fp8_workspace_bytes(1, 16, 24, ctypes.byref(out)) == -2                                 # K not a multiple of 16
+    assert L.slim_fp8_workspace_bytes(1, 1 << 21, 16, ctypes.byref(out)) == -2
+    quant = lambda W=a, type_=1, ld=256, codes=a, scales=a, N=128, K=256: L.slim_fp8_quantize(W, type_, ld, codes, scales, N, K, None)
+    assert quant(type_=5) == -1 and quant(ld=255) == -1 and quant(W=None) == -1 and quant(codes=None) == -1 and quant(scales=None) == -1
+    assert quant(K=250) == -2 and quant(N=-1) == -1 and quant(N=0) == 0
+    assert quant(W=a + 2) == -3 and quant(ld=260) == -3
+    lin = lambda x=a, xt=1, ldx=256, codes=a, scales=a, y=a, yt=1, ldy=128, M=4, N=128, K=256, ws=a, wb=4096: L.slim_fp8_linear(
+        x, xt, ldx, codes, scales, y, yt, ldy, M, N, K, ws, wb, None)
+    assert lin(M=0) == 0 and lin(N=0, ldy=0) == 0
+    assert lin(M=-1) == -1 and lin(xt=0) == -1 and lin(yt=2) == -1 and lin(ldx=255) == -1 and lin(ldy=127) == -1
+    assert lin(x=None) == -1 and lin(y=None) == -1 and lin(codes=None) == -1 and lin(scales=None) == -1
+    assert lin(K=248) == -2
+    assert lin(x=a + 2) == -3 and lin(ldx=260) == -3 and lin(y=a + 4) == -3 and lin(ws=a + 8) == -3
+    assert lin(ws=None) == -4 and lin(wb=100) == -4 and lin(M=64) == -4                                   # staged x does not fit 4096 bytes
