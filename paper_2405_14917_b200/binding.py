@@ -3,8 +3,8 @@
 Argument marshalling only: every function checks dtypes/devices, takes raw device
 pointers from torch tensors and the current CUDA stream, and calls the entry point
 of the same name; for the linear layers and the layer sets, which a decode loop calls
-per layer, the host module (csrc/slim_host.cpp) does that without the interpreter, where
-it has been built for the running torch.
+per layer, and the distillation loss the host module (csrc/slim_host.cpp) does that without
+the interpreter, where it has been built for the running torch.
 There is no fallback: if the CUDA library has not been built the first call raises.
 """
 from __future__ import annotations
@@ -106,6 +106,14 @@ class _NoHost:
     def run_set(*_):
         return None
 
+    @staticmethod
+    def fp8_linear(*_):
+        return None
+
+    @staticmethod
+    def distill(*_):
+        return None
+
 
 def host():
     """Loads the host module (built with the CUDA library); without it calls only take longer on the host."""
@@ -119,7 +127,8 @@ def host():
         except ImportError as e:
             warnings.warn(f"host module not loaded ({e}); `python -m paper_2405_14917_b200.build` builds it for this torch")
             module = _NoHost
-        for name in ("slim_mpq_gemv", "slim_mpq_gemm", "slim_mpq_gemv_set"):
+        for name in ("slim_mpq_gemv", "slim_mpq_gemm", "slim_mpq_gemv_set", "slim_fp8_linear", "slim_distill_loss", "slim_distill_grad",
+                     "slim_distill_step"):
             _entry[name] = ctypes.cast(getattr(L, name), ctypes.c_void_p).value
         _host = module
     return _host
@@ -408,6 +417,12 @@ def fp8_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, works
                out_dtype: torch.dtype | None = None) -> torch.Tensor:
     """y = x W^T with W in e4m3 under a scale per block of 128 x 128, x (fp16 or bf16 [M][K], rows may be strided) quantised
     inside the call (slim_fp8_linear).  y is of x's type, or fp32 (out_dtype, or out's)."""
+    y = (_host or host()).fp8_linear(_entry["slim_fp8_linear"], x, codes, scales, workspace, out, -1 if out_dtype is None else _TYPES.get(out_dtype, 3))
+    if y is not None:
+        if type(y) is int:
+            _check("slim_fp8_linear", y)
+        return y
+    # not the plain call: raise, or go through Python
     ldx = _rows(x, "x", (torch.float16, torch.bfloat16))
     M, K = x.shape
     cp, sp, wp = _dev(codes, torch.float8_e4m3fn, "codes"), _dev(scales, torch.float32, "scales"), _dev(workspace, torch.uint8, "workspace")
@@ -429,6 +444,13 @@ def fp8_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, works
         _check("slim_fp8_linear", lib().slim_fp8_linear(x.data_ptr(), _TYPES[x.dtype], ldx, cp, sp, out.data_ptr(), _TYPES[out.dtype], ldy, M, N, K,
                                                         wp, workspace.numel(), _stream(x)))
     return out
+
+
+def _distill_host(fn_name: str, mode: int, logits, top_index, top_logit, teacher_lse, temperature, saved=None, dloss=None, out=None):
+    r = (_host or host()).distill(_entry[fn_name], mode, logits, top_index, top_logit, teacher_lse, float(temperature), saved, dloss, out)
+    if type(r) is int:
+        _check(fn_name, r)
+    return r
 
 
 def _distill_args(logits, top_index, top_logit, temperature, teacher_lse):
@@ -463,6 +485,9 @@ def distill_loss(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch
     (fp32, fp16 or bf16, rows may be strided), top_index int32/int64 [M][k] (outside [0, V): absent), top_logit [M][k].
     teacher_lse fp32 [M]: the log-sum-exp of the teacher's whole row / temperature, and then the columns outside
     the entries count as one more class.  Returns (loss fp32 [M], saved), saved being what distill_grad needs."""
+    r = _distill_host("slim_distill_loss", 0, logits, top_index, top_logit, teacher_lse, temperature)
+    if r is not None:
+        return r
     args = _distill_args(logits, top_index, top_logit, temperature, teacher_lse)
     M = logits.shape[0]
     loss = torch.empty(M, dtype=torch.float32, device=logits.device)
@@ -476,6 +501,9 @@ def distill_grad(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch
                  temperature: float = 1.0, teacher_lse: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient of sum(dloss * loss) with respect to the logits, from what distill_loss saved for the same arguments
     (slim_distill_grad).  dloss fp32 [M]; out may be the logits themselves."""
+    r = _distill_host("slim_distill_grad", 1, logits, top_index, top_logit, teacher_lse, temperature, saved, dloss, out)
+    if r is not None:
+        return r
     args = _distill_args(logits, top_index, top_logit, temperature, teacher_lse)
     M = logits.shape[0]
     sp = _vector(saved, 4 * M, torch.float32, "saved", logits.device)
@@ -490,6 +518,9 @@ def distill_step(logits: torch.Tensor, top_index: torch.Tensor, top_logit: torch
                  teacher_lse: torch.Tensor | None = None, out: torch.Tensor | None = None):
     """distill_loss and distill_grad in one pass over the logits, for a loss whose weights dloss (fp32 [M]) are known
     beforehand (slim_distill_step).  Returns (loss fp32 [M], gradient); out may be the logits themselves."""
+    r = _distill_host("slim_distill_step", 2, logits, top_index, top_logit, teacher_lse, temperature, None, dloss, out)
+    if r is not None:
+        return r
     args = _distill_args(logits, top_index, top_logit, temperature, teacher_lse)
     M = logits.shape[0]
     dp = _vector(dloss, M, torch.float32, "dloss", logits.device)
