@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(256) fp8_quantize_kernel(const T* __restrict__
 // Half a warp per block of 128 columns of a token, 8 columns per lane.  The kernel that reads the codes may be set up meanwhile.
 template <typename T>
 __global__ void __launch_bounds__(256) fp8_stage_kernel(const T* __restrict__ x, long long ld, uint8_t* __restrict__ codes,
-                                                        float* __restrict__ scales, int M, int K, int G, int Mp) {
+                                                        uint8_t* __restrict__ scales, int M, int K, int G, int Mp) {
     pdl_launch_dependents();
     pdl_wait();
     const long long unit = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) >> 4;
@@ -80,10 +80,10 @@ __global__ void __launch_bounds__(256) fp8_stage_kernel(const T* __restrict__ x,
     const uint32_t sb = f8::scale_bits(mx);
     const float inv = f8::inverse_scale(sb);
     if (in) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(m) * K + k) = make_uint2(f8::codes4(f, inv), f8::codes4(f + 4, inv));
-    if (c == 0 && m < M) scales[static_cast<size_t>(g) * Mp + m] = __uint_as_float(sb);
+    if (c == 0 && m < M) scales[(static_cast<size_t>(g >> 2) * Mp + m) * 4 + (g & 3)] = static_cast<uint8_t>(sb >> 23);
 }
 
-static cudaError_t fp8_stage(const Fp8Args& a, uint8_t* codes, float* scales, int Mp) {
+static cudaError_t fp8_stage(const Fp8Args& a, uint8_t* codes, uint8_t* scales, int Mp) {
     const int G = (a.K + f8::kBlock - 1) / f8::kBlock;
     const long long units = static_cast<long long>(a.M) * G;
     PdlLaunch l(static_cast<unsigned>((units + 15) / 16), 256, 0, a.stream);
@@ -178,9 +178,9 @@ extern "C" int slim_fp8_linear(const void* x, int x_type, long long ldx, const v
     a.stream = s;
     if (!slim::fp8_few_takes_x(M)) {
         const slim::Fp8Staging sg = slim::fp8_staging(M, K);
-        SLIM_CUDA_TRY(slim::fp8_stage(a, a.workspace + sg.codes, reinterpret_cast<float*>(a.workspace + sg.scales), sg.Mp));
+        SLIM_CUDA_TRY(slim::fp8_stage(a, a.workspace + sg.codes, a.workspace + sg.scales, sg.Mp));
         a.x_codes = a.workspace + sg.codes;
-        a.x_scales = reinterpret_cast<const float*>(a.workspace + sg.scales);
+        a.x_scales = reinterpret_cast<const uint32_t*>(a.workspace + sg.scales);
         a.Mp = sg.Mp;
     }
     SLIM_CUDA_TRY(slim::fp8_use_gemm(M, N, K) ? slim::fp8_gemm(a) : slim::fp8_few(a));

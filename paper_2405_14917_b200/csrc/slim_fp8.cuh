@@ -84,21 +84,6 @@ __device__ __forceinline__ void ld16(uint32_t taddr, uint32_t* v) {
           "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {      // two fp32 multiply-adds
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t pack2(uint32_t a, uint32_t b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
-    return r;
-}
-__device__ __forceinline__ float2 unpack2(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
 // Waits, for a millisecond at most and whatever the other roles do, until a barrier's phase completes: what is in flight when a call
 // gives up has landed before its shared memory goes.
 __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
@@ -109,17 +94,17 @@ __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
 }  // namespace f8
 
 // Where the quantised activations of a call lie in its workspace: behind the header and the flags of the other calls, which
-// are left alone, the codes [M][K], then the scales [groups][Mp], Mp = M rounded up to 32.
+// are left alone, the codes [M][K], then the scales' exponents, a word of four groups per token, [groups / 4][Mp], Mp = M rounded up to 128.
 struct Fp8Staging {
     size_t codes, scales, bytes;
     int Mp;
 };
 inline Fp8Staging fp8_staging(int M, int K) {
     Fp8Staging s;
-    s.Mp = (M + 31) / 32 * 32;
+    s.Mp = (M + 127) / 128 * 128;
     s.codes = kWsFlagsOffset + kWsFlagsBytes;
     s.scales = (s.codes + static_cast<size_t>(M) * K + 255) / 256 * 256;
-    s.bytes = s.scales + static_cast<size_t>((K + f8::kBlock - 1) / f8::kBlock) * s.Mp * sizeof(float);
+    s.bytes = s.scales + static_cast<size_t>((K + 4 * f8::kBlock - 1) / (4 * f8::kBlock)) * s.Mp * sizeof(uint32_t);
     return s;
 }
 
@@ -135,7 +120,7 @@ struct Fp8Args {
     int M, N, K;
     uint8_t* workspace;
     const uint8_t* x_codes;   // staged
-    const float* x_scales;
+    const uint32_t* x_scales;
     int Mp;
     cudaStream_t stream;
 };

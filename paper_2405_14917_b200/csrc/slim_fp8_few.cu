@@ -36,7 +36,7 @@ template <int T> struct FewCfg {
 struct FewParams {
     const void* x;
     long long ldx;
-    const float* x_scales;       // staged: [G][Mp]
+    const uint8_t* x_scales;     // staged: exponents, byte g % 4 of word [g / 4][token]
     const float* scales;
     void* y;
     long long ldy;
@@ -189,7 +189,7 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                 if (!tc::warp_wait(x_empty(s), ph ^ 1u, abort)) break;
 #pragma unroll
                 for (int t = lane; t < T; t += 32)
-                    *reinterpret_cast<float*>(smem + C::OFF_SX + 4 * (s * T + t)) = t < tokens ? __ldcg(p.x_scales + static_cast<size_t>(g0 + i) * p.Mp + m0 + t) : 0.f;
+                    *reinterpret_cast<float*>(smem + C::OFF_SX + 4 * (s * T + t)) = t < tokens ? __uint_as_float(static_cast<uint32_t>(__ldcg(p.x_scales + (static_cast<size_t>((g0 + i) >> 2) * p.Mp + m0 + t) * 4 + ((g0 + i) & 3))) << 23) : 0.f;
                 __syncwarp();
                 if (lane == 0) sb::arrive(x_full(s));
             }
@@ -314,7 +314,7 @@ static cudaError_t few_launch(const Fp8Args& a) {
     }
     FewParams p;
     memset(&p, 0, sizeof p);
-    p.x = a.x; p.ldx = a.ldx; p.x_scales = a.x_scales; p.scales = a.scales; p.y = a.y; p.ldy = a.ldy;
+    p.x = a.x; p.ldx = a.ldx; p.x_scales = reinterpret_cast<const uint8_t*>(a.x_scales); p.scales = a.scales; p.y = a.y; p.ldy = a.ldy;
     p.status = reinterpret_cast<unsigned int*>(a.workspace);
     p.y_type = a.y_type; p.M = a.M; p.N = a.N; p.K = a.K; p.G = (a.K + f8::kBlock - 1) / f8::kBlock; p.Mp = a.Mp;
     CUtensorMap w_map, x_map;

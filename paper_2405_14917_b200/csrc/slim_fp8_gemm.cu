@@ -1,35 +1,44 @@
-// The 8-bit linear layer for many tokens: CTA pairs, 256 tokens x 256 output features per tile.
+// The 8-bit linear layer for many tokens: CTA pairs, 256 tokens x up to 256 output features per tile.
 //
 // Bound: the tensor cores.  One tcgen05.mma (cta_group::2, e4m3) of a pair takes 256 tokens (128 of each CTA, the M dimension: a
-// tensor-memory lane is a token) times 256 rows of W (half from each CTA's shared memory) over 32 columns.  The scales change every 128
-// columns, so the four MMAs of a block start a new accumulator and its sums go, while the next block's MMAs fill the other
-// half of tensor memory, into fp32 registers under the block's scale:  acc += d * (sx[token] * sw[128 features]).  A thread owns
-// one token and 128 features, so both scales are one number per thread and block, and the step costs 64 packed multiply-adds
-// per thread, 2 x 64 of 512 issue slots that the block's MMAs take on an SM.
+// tensor-memory lane is a token) times up to 256 rows of W (half from each CTA's shared memory) over 32 columns.  All scales are powers of two, so the
+// block-scaled form (kind::mxf8f6f4, E8M0 scales of 32 columns each) applies them inside the MMA: the four MMAs of a block of 128 columns name the
+// same byte of a row's scale word, and a tile's sum over all of K stays in tensor memory.  Plain MMAs with a pass over D per block (into
+// registers, under the block's scale) reached 2.1 PFLOP/s at 2048 x 13824 x 5120 in the best of four forms: reading D competes with
+// the MMAs' own accumulation (430 to 550 cycles per block beside them, 150 alone, of 512 that its MMAs take).
 //
-// Warps of a CTA (10): 0 TMA of its 128 tokens and 128 rows of W per block into a ring of 32 KB slots; 1 in the leader the
-// MMAs, in the other CTA the relay that tells the leader its half has landed; 2 to 9 sums and output.  Persistent pairs; every wait is bounded and
-// reports through the workspace status word.
+// Scale words (four blocks' bytes) go to tensor memory by tcgen05.st: row r's word at lane r % 32 of column r / 32, the same in all four lane
+// quarters; two buffers.  A CTA has the words of its own tokens and of all features.
+//
+// Warps of a CTA (16): 0 TMA of its 128 tokens and its half of the rows of W per block into a ring of 32 KB slots; 1 in the leader the
+// MMAs, in the other CTA the relay that tells the leader its half has landed; 4 to 7 scale words; 8 to 15 output: they take D into
+// registers at once, so that the next tile's MMAs wait for the reading alone, and convert and store beside them.
+// Persistent pairs; every wait is bounded and reports through the workspace status word.
 #include "slim_fp8.cuh"
 
 #include <atomic>
 
 namespace slim {
 
-constexpr int kFgThreads = 320;
-constexpr int kFgTok = 256, kFgFeat = 256;         // of a pair's tile; each CTA: 128 tokens, and brings 128 rows of W
+constexpr int kFgThreads = 512;
+// Registers after the split: 256 x 80 + 256 x 176 = 512 x 128, what the block is launched with.
+constexpr int kFgRegsFew = 80, kFgRegsMany = 176;
+constexpr int kFgTok = 256, kFgFeat = 256;         // of a pair's tile, at most; each CTA: 128 tokens, and brings half of the rows of W
 constexpr int kFgStages = 6;
 constexpr int kFgSlot = 2 * 128 * 128;
 constexpr int kFgOffBar = kFgStages * kFgSlot;
 constexpr int kFgSmem = kFgOffBar + 256 + 1024;
+constexpr int kFgColScales = kFgFeat;              // tensor memory: D, then two buffers of 4 + 8 columns of scale words
+constexpr int kFgScaleCols = 16;
 
 struct FgParams {
-    const float* x_scales;       // [G][Mp]
+    const uint32_t* x_scales;    // [ceil(G / 4)][Mp]
     const float* scales;         // [ceil(N / 128)][G]
     void* y;
     long long ldy;
     unsigned int* status;
     int y_type, M, N, G, Mp;
+    int feat;                    // features of a tile, a multiple of 32
     int tok_tiles, tiles;
 };
 
@@ -53,11 +62,20 @@ __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"(static_cast<uint16_t>(3)) : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// D (+)= A B^T over the pair, e4m3, the products of every row of A and of B times the row's scale.
+__device__ __forceinline__ void mma_scaled(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+}
+// Instruction descriptor: e4m3 operands, both K-major, E8M0 scales from byte `id` of their words, m x n.
+__device__ __forceinline__ uint32_t idesc_scaled(int m, int n, int id) {
+    return (static_cast<uint32_t>(id) << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (1u << 23) | (static_cast<uint32_t>(m >> 7) << 27) |
+           (static_cast<uint32_t>(id) << 29);
+}
+__device__ __forceinline__ void st4(uint32_t taddr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 }  // namespace fg
 
@@ -69,21 +87,24 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     auto full = [&](int s) { return bars + 8u * s; };                         // this CTA's slot has landed
     auto peer = [&](int s) { return bars + 8u * (kFgStages + s); };           // leader's: the other CTA's has
     auto empty = [&](int s) { return bars + 8u * (2 * kFgStages + s); };
-    auto d_full = [&](int b) { return bars + 8u * (3 * kFgStages + b); };
-    auto d_empty = [&](int b) { return bars + 8u * (3 * kFgStages + 2 + b); };    // leader's: the sums' warps of both CTAs
-    static_assert(8 * (3 * kFgStages + 4) <= 240, "room for the barriers");
+    auto sf_full = [&](int b) { return bars + 8u * (3 * kFgStages + b); };    // leader's: the scale warps of both CTAs
+    auto sf_empty = [&](int b) { return bars + 8u * (3 * kFgStages + 2 + b); };
+    const uint32_t d_full = bars + 8u * (3 * kFgStages + 4), d_empty = d_full + 8u;      // d_empty: leader's, the output warps of both CTAs
+    static_assert(8 * (3 * kFgStages + 6) <= 240, "room for the barriers");
     volatile int* abort = reinterpret_cast<volatile int*>(smem + kFgOffBar + 240);
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + kFgOffBar + 244);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(tc::uniform(tid >> 5));
     const int rank = static_cast<int>(cluster_ctarank());
     const int pair = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
-    const int G = p.G;
+    const int G = p.G, feat = p.feat;
 
     if (tid == 0) {
         *abort = 0;
         for (int s = 0; s < kFgStages; ++s) { sb::init(full(s), 1); sb::init(peer(s), 1); sb::init(empty(s), 1); }
-        for (int b = 0; b < 2; ++b) { sb::init(d_full(b), 1); sb::init(d_empty(b), 16); }
+        for (int b = 0; b < 2; ++b) { sb::init(sf_full(b), 8); sb::init(sf_empty(b), 1); }
+        sb::init(d_full, 1);
+        sb::init(d_empty, 16);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -99,111 +120,140 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     pdl_wait();
 
     int issued = 0;                                    // blocks this role has begun
-    if (warp == 0) {
-        for (int tile = pair; tile < p.tiles; tile += pairs) {
-            const int m0 = tile % p.tok_tiles * kFgTok + 128 * rank, n0 = tile / p.tok_tiles * kFgFeat + 128 * rank;
-            int g = 0;
-            for (; g < G; ++g, ++issued) {
-                const int s = issued % kFgStages;
-                if (!tc::warp_wait(empty(s), ((issued / kFgStages) & 1u) ^ 1u, abort)) break;
-                if (tc::elect()) {
-                    sb::expect_tx(full(s), kFgSlot);
-                    tc::tma_load_2d(base + s * kFgSlot, &x_map, 128 * g, m0, full(s));
-                    tc::tma_load_2d(base + s * kFgSlot + kFgSlot / 2, &w_map, 128 * g, n0, full(s));
-                }
-                __syncwarp();
-            }
-            if (g < G) break;
-        }
-    } else if (warp == 1) {
-        for (int tile = pair; tile < p.tiles; tile += pairs) {
-            int g = 0;
-            for (; g < G; ++g, ++issued) {
-                const int s = issued % kFgStages, b = issued & 1;
-                const uint32_t ph = (issued / kFgStages) & 1u;
-                if (!tc::warp_wait(full(s), ph, abort)) break;
-                if (rank != 0) {
-                    if (tc::elect()) fg::arrive_cluster(fg::map_to_cta(peer(s), 0));
+    if (warp < 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFgRegsFew));
+        if (warp == 0) {
+            const uint32_t bytes = (128u + static_cast<uint32_t>(feat) / 2u) * 128u;
+            for (int tile = pair; tile < p.tiles; tile += pairs) {
+                const int m0 = tile % p.tok_tiles * kFgTok + 128 * rank, n0 = tile / p.tok_tiles * feat + feat / 2 * rank;
+                int g = 0;
+                for (; g < G; ++g, ++issued) {
+                    const int s = issued % kFgStages;
+                    if (!tc::warp_wait(empty(s), ((issued / kFgStages) & 1u) ^ 1u, abort)) break;
+                    if (tc::elect()) {
+                        sb::expect_tx(full(s), bytes);
+                        tc::tma_load_2d(base + s * kFgSlot, &x_map, 128 * g, m0, full(s));
+                        tc::tma_load_2d(base + s * kFgSlot + kFgSlot / 2, &w_map, 128 * g, n0, full(s));
+                    }
                     __syncwarp();
-                    continue;
                 }
-                if (!tc::warp_wait(peer(s), ph, abort)) break;
-                if (!tc::warp_wait(d_empty(b), ((issued >> 1) & 1u) ^ 1u, abort)) break;
-                tc::fence_after();
-                const uint64_t a = tc::desc_k128(base + s * kFgSlot), w = tc::desc_k128(base + s * kFgSlot + kFgSlot / 2);
-                if (tc::elect()) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) fg::mma_ss(tmem + b * kFgFeat, a + 2 * k, w + 2 * k, f8::idesc(kFgTok, kFgFeat), k > 0 ? 1u : 0u);
-                    fg::commit(empty(s));
-                    fg::commit(d_full(b));
-                }
-                __syncwarp();
+                if (g < G) break;
             }
-            if (g < G) break;
+        } else if (warp == 1) {
+            int words = 0;                             // groups of four blocks begun
+            uint32_t tiles_done = 0;
+            for (int tile = pair; tile < p.tiles; tile += pairs, ++tiles_done) {
+                int g = 0;
+                if (rank == 0 && !tc::warp_wait(d_empty, (tiles_done & 1u) ^ 1u, abort)) break;
+                for (; g < G; ++g, ++issued) {
+                    const int s = issued % kFgStages;
+                    const uint32_t ph = (issued / kFgStages) & 1u;
+                    if (!tc::warp_wait(full(s), ph, abort)) break;
+                    if (rank != 0) {
+                        if (tc::elect()) fg::arrive_cluster(fg::map_to_cta(peer(s), 0));
+                        __syncwarp();
+                        continue;
+                    }
+                    if (!tc::warp_wait(peer(s), ph, abort)) break;
+                    const int b = words & 1;
+                    if ((g & 3) == 0 && !tc::warp_wait(sf_full(b), (words >> 1) & 1u, abort)) break;
+                    tc::fence_after();
+                    const uint64_t a = tc::desc_k128(base + s * kFgSlot), w = tc::desc_k128(base + s * kFgSlot + kFgSlot / 2);
+                    const uint32_t idesc = fg::idesc_scaled(kFgTok, feat, g & 3), sa = tmem + kFgColScales + kFgScaleCols * b;
+                    const bool last = (g & 3) == 3 || g + 1 == G;
+                    if (tc::elect()) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) fg::mma_scaled(tmem, a + 2 * k, w + 2 * k, idesc, sa, sa + 4, g > 0 || k > 0 ? 1u : 0u);
+                        fg::commit(empty(s));
+                        if (last) fg::commit(sf_empty(b));
+                        if (g + 1 == G) fg::commit(d_full);
+                    }
+                    __syncwarp();
+                    if (last) ++words;
+                }
+                if (g < G) break;
+            }
+        } else if (warp >= 4) {
+            // ---- scale words: this warp's quarter of the lanes, of all of the CTA's tokens and the tile's features
+            const int q = warp & 3;
+            const uint32_t sf_t = tmem + kFgColScales + (static_cast<uint32_t>(32 * q) << 16);
+            const uint32_t sf_full_leader = fg::map_to_cta(sf_full(0), 0);
+            const int n_blocks = (p.N + 127) / 128;
+            bool ok = true;
+            for (int tile = pair; tile < p.tiles && ok; tile += pairs) {
+                const int m0 = min(tile % p.tok_tiles * kFgTok + 128 * rank, p.Mp - 128), nb0 = tile / p.tok_tiles * feat;
+                for (int g = 0; g < G; g += 4, ++issued) {
+                    const int b = issued & 1;
+                    uint32_t xw[4], ww[8];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) xw[c] = __ldcg(p.x_scales + static_cast<size_t>(g >> 2) * p.Mp + m0 + 32 * c + lane);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {      // 32 features of column c lie in one block of 128
+                        const float* sw = p.scales + static_cast<size_t>(min((nb0 + 32 * c) >> 7, n_blocks - 1)) * G + g;
+                        uint32_t v = 0;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (g + e < G) v |= (__float_as_uint(__ldg(sw + e)) >> 23 & 0xffu) << (8 * e);
+                        ww[c] = v;
+                    }
+                    ok = tc::warp_wait(sf_empty(b), ((issued >> 1) & 1u) ^ 1u, abort);
+                    if (!ok) break;
+                    tc::fence_after();
+                    fg::st4(sf_t + kFgScaleCols * b, xw);
+                    tc::st8(sf_t + kFgScaleCols * b + 4, ww);
+                    tc::wait_st();
+                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) fg::arrive_cluster(sf_full_leader + 8u * b);
+                }
+            }
         }
     } else {
-        const int half = (warp - 2) >> 2, q = warp & 3;
-        const uint32_t d_t = tmem + 128u * half + (static_cast<uint32_t>(32 * q) << 16);
-        const uint32_t d_empty_leader = fg::map_to_cta(d_empty(0), 0);
-        const int n_blocks = (p.N + 127) / 128;
-        for (int tile = pair; tile < p.tiles; tile += pairs) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kFgRegsMany));
+        const int half = (warp - 8) >> 2, q = warp & 3, cols = feat / 2;
+        const uint32_t d_t = tmem + static_cast<uint32_t>(cols * half) + (static_cast<uint32_t>(32 * q) << 16);
+        const uint32_t d_empty_leader = fg::map_to_cta(d_empty, 0);
+        uint32_t ph = 0;
+        for (int tile = pair; tile < p.tiles; tile += pairs, ph ^= 1u) {
             const int token = tile % p.tok_tiles * kFgTok + 128 * rank + 32 * q + lane;
-            const int n0 = tile / p.tok_tiles * kFgFeat + 128 * half;
-            const float* sx = p.x_scales + min(token, p.M - 1);
-            const float* sw = p.scales + static_cast<size_t>(min(n0 / 128, n_blocks - 1)) * G;
-            uint64_t acc[64];
+            const int n0 = tile / p.tok_tiles * feat + cols * half;
+            uint32_t d[8][16];
+            if (!tc::warp_wait(d_full, ph, abort)) break;
+            tc::fence_after();
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = 0ull;
-            float x_next = __ldcg(sx), w_next = __ldg(sw);
-            int g = 0;
-            for (; g < G; ++g, ++issued) {
-                const int b = issued & 1;
-                const float sc = x_next * w_next;
-                if (g + 1 < G) { x_next = __ldcg(sx + static_cast<size_t>(g + 1) * p.Mp); w_next = __ldg(sw + g + 1); }
-                const uint64_t sc2 = f8::pack2(__float_as_uint(sc), __float_as_uint(sc));
-                if (!tc::warp_wait(d_full(b), (issued >> 1) & 1u, abort)) break;
-                tc::fence_after();
-#pragma unroll
-                for (int c = 0; c < 128; c += 16) {
-                    uint32_t d[16];
-                    f8::ld16(d_t + b * kFgFeat + c, d);
-                    tc::wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[c / 2 + i] = f8::fma2(f8::pack2(d[2 * i], d[2 * i + 1]), sc2, acc[c / 2 + i]);
-                }
-                tc::fence_before();
-                __syncwarp();
-                if (lane == 0) fg::arrive_cluster(d_empty_leader + 8u * b);
-            }
-            if (g < G) break;
-            if (token < p.M && n0 < p.N) {
+            for (int c = 0; c < 8; ++c)
+                if (16 * c < cols) f8::ld16(d_t + 16 * c, d[c]);
+            tc::wait_ld();
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) fg::arrive_cluster(d_empty_leader);
+            if (token < p.M) {
                 const size_t at = static_cast<size_t>(token) * p.ldy + n0;
-                const int n = min(128, p.N - n0);
-                const bool whole = n == 128 && p.ldy % 8 == 0;          // y is 16-byte aligned
-                if (whole && p.y_type == SLIM_F32) {
 #pragma unroll
-                    for (int i = 0; i < 64; i += 2) {
-                        const float2 u = f8::unpack2(acc[i]), v = f8::unpack2(acc[i + 1]);
-                        *reinterpret_cast<float4*>(static_cast<float*>(p.y) + at + 2 * i) = make_float4(u.x, u.y, v.x, v.y);
-                    }
-                } else if (whole) {
+                for (int c = 0; c < 8; ++c) {
+                    const int n = min(16, min(cols, p.N - n0) - 16 * c);
+                    if (n <= 0) break;
+                    const float* v = reinterpret_cast<const float*>(d[c]);
+                    if (n == 16 && p.ldy % 8 == 0) {   // y is 16-byte aligned, and so is n0
+                        if (p.y_type == SLIM_F32) {
 #pragma unroll
-                    for (int i = 0; i < 64; i += 4) {
-                        uint32_t w[4];
+                            for (int i = 0; i < 16; i += 4)
+                                *reinterpret_cast<float4*>(static_cast<float*>(p.y) + at + 16 * c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                        } else {
+                            uint32_t w[8];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float2 u = f8::unpack2(acc[i + j]);
-                            if (p.y_type == SLIM_F16) { const __half2 h = __floats2half2_rn(u.x, u.y); w[j] = *reinterpret_cast<const uint32_t*>(&h); }
-                            else { const __nv_bfloat162 h = __floats2bfloat162_rn(u.x, u.y); w[j] = *reinterpret_cast<const uint32_t*>(&h); }
+                            for (int i = 0; i < 8; ++i) {
+                                if (p.y_type == SLIM_F16) { const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
+                                else { const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
+                            }
+                            uint4* o = reinterpret_cast<uint4*>(static_cast<__half*>(p.y) + at + 16 * c);
+                            o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+                            o[1] = make_uint4(w[4], w[5], w[6], w[7]);
                         }
-                        *reinterpret_cast<uint4*>(static_cast<__half*>(p.y) + at + 2 * i) = make_uint4(w[0], w[1], w[2], w[3]);
-                    }
-                } else {
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i) {
-                        const float2 u = f8::unpack2(acc[i]);
-                        if (2 * i < n) f8::store_y(p.y, p.y_type, at + 2 * i, u.x);
-                        if (2 * i + 1 < n) f8::store_y(p.y, p.y_type, at + 2 * i + 1, u.y);
+                        for (int i = 0; i < 16; ++i)
+                            if (i < n) f8::store_y(p.y, p.y_type, at + 16 * c + i, v[i]);
                     }
                 }
             }
@@ -217,8 +267,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
             __syncwarp();
         }
     if (warp == 1 && rank == 0 && *abort != 0)
-        for (int i = max(0, issued - 2); i < issued; ++i) {
-            if (tc::elect()) f8::drain(d_full(i & 1), (i >> 1) & 1u);
+        for (int i = max(0, issued - kFgStages); i < issued; ++i) {
+            if (tc::elect()) f8::drain(empty(i % kFgStages), (i / kFgStages) & 1u);
             __syncwarp();
         }
     tc::fence_before();
@@ -246,10 +296,11 @@ cudaError_t fp8_gemm(const Fp8Args& a) {
     p.status = reinterpret_cast<unsigned int*>(a.workspace);
     p.y_type = a.y_type; p.M = a.M; p.N = a.N; p.G = (a.K + f8::kBlock - 1) / f8::kBlock; p.Mp = a.Mp;
     p.tok_tiles = (a.M + kFgTok - 1) / kFgTok;
-    p.tiles = p.tok_tiles * ((a.N + kFgFeat - 1) / kFgFeat);
-    CUtensorMap x_map, w_map;
-    if (!make_byte_map(&x_map, a.x_codes, a.M, a.K, 128) || !make_byte_map(&w_map, a.codes, a.N, a.K, 128)) return cudaErrorUnknown;
     const int pairs = device_sm_count() / 2;
+    p.feat = kFgFeat;
+    p.tiles = p.tok_tiles * ((a.N + p.feat - 1) / p.feat);
+    CUtensorMap x_map, w_map;
+    if (!make_byte_map(&x_map, a.x_codes, a.M, a.K, 128) || !make_byte_map(&w_map, a.codes, a.N, a.K, p.feat / 2)) return cudaErrorUnknown;
     PdlLaunch l(static_cast<unsigned>(2 * (p.tiles < pairs ? p.tiles : pairs)), kFgThreads, kFgSmem, a.stream);      // clusters of 2: see the kernel
     return cudaLaunchKernelEx(&l.cfg, fp8_gemm_kernel, x_map, w_map, p);
 }
