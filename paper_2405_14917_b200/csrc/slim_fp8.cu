@@ -57,39 +57,49 @@ __global__ void __launch_bounds__(256) fp8_quantize_kernel(const T* __restrict__
 }
 
 // ------------------------------------------------------------------------------------------ x
-// Half a warp per block of 128 columns of a token, 8 columns per lane.  The kernel that reads the codes may be set up meanwhile.
+// Half a warp per four blocks of 128 columns of a token, 8 columns of each per lane: four loads in flight per thread and one word of
+// scale exponents (1280 blocks of threads at 2048 x 5120, one wave).  The kernel that reads the codes may be set up meanwhile.
 template <typename T>
 __global__ void __launch_bounds__(256) fp8_stage_kernel(const T* __restrict__ x, long long ld, uint8_t* __restrict__ codes,
-                                                        uint8_t* __restrict__ scales, int M, int K, int G, int Mp) {
+                                                        uint32_t* __restrict__ scales, int M, int K, int words, int Mp) {
     pdl_launch_dependents();
     pdl_wait();
     const long long unit = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) >> 4;
     const int c = threadIdx.x & 15;
-    const int m = static_cast<int>(unit / G), g = static_cast<int>(unit - static_cast<long long>(m) * G);
-    const int k = g * f8::kBlock + 8 * c;
-    float f[8];
+    const int m = static_cast<int>(unit / words), j = static_cast<int>(unit - static_cast<long long>(m) * words);
+    const T* row = x + static_cast<size_t>(m) * ld;
+    uint4 v[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = 0.f;
-    const bool in = m < M && k < K;
-    if (in) f8::unpack8<T>(*reinterpret_cast<const uint4*>(x + static_cast<size_t>(m) * ld + k), f);
-    uint32_t mx = 0;
+    for (int i = 0; i < 4; ++i) {
+        const int k = (4 * j + i) * f8::kBlock + 8 * c;
+        v[i] = m < M && k < K ? __ldg(reinterpret_cast<const uint4*>(row + k)) : make_uint4(0, 0, 0, 0);
+    }
+    uint32_t word = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) mx = max(mx, f8::magnitude(f[e]));
+    for (int i = 0; i < 4; ++i) {
+        const int k = (4 * j + i) * f8::kBlock + 8 * c;
+        float f[8];
+        f8::unpack8<T>(v[i], f);
+        uint32_t mx = 0;
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    const uint32_t sb = f8::scale_bits(mx);
-    const float inv = f8::inverse_scale(sb);
-    if (in) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(m) * K + k) = make_uint2(f8::codes4(f, inv), f8::codes4(f + 4, inv));
-    if (c == 0 && m < M) scales[(static_cast<size_t>(g >> 2) * Mp + m) * 4 + (g & 3)] = static_cast<uint8_t>(sb >> 23);
+        for (int e = 0; e < 8; ++e) mx = max(mx, f8::magnitude(f[e]));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const uint32_t sb = f8::scale_bits(mx);
+        const float inv = f8::inverse_scale(sb);
+        if (m < M && k < K) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(m) * K + k) = make_uint2(f8::codes4(f, inv), f8::codes4(f + 4, inv));
+        word |= (sb >> 23) << (8 * i);
+    }
+    if (c == 0 && m < M) scales[static_cast<size_t>(j) * Mp + m] = word;
 }
 
-static cudaError_t fp8_stage(const Fp8Args& a, uint8_t* codes, uint8_t* scales, int Mp) {
-    const int G = (a.K + f8::kBlock - 1) / f8::kBlock;
-    const long long units = static_cast<long long>(a.M) * G;
+static cudaError_t fp8_stage(const Fp8Args& a, uint8_t* codes, uint32_t* scales, int Mp) {
+    const int words = (a.K + 4 * f8::kBlock - 1) / (4 * f8::kBlock);
+    const long long units = static_cast<long long>(a.M) * words;
     PdlLaunch l(static_cast<unsigned>((units + 15) / 16), 256, 0, a.stream);
     if (a.x_type == SLIM_F16)
-        return cudaLaunchKernelEx(&l.cfg, fp8_stage_kernel<__half>, static_cast<const __half*>(a.x), a.ldx, codes, scales, a.M, a.K, G, Mp);
-    return cudaLaunchKernelEx(&l.cfg, fp8_stage_kernel<__nv_bfloat16>, static_cast<const __nv_bfloat16*>(a.x), a.ldx, codes, scales, a.M, a.K, G, Mp);
+        return cudaLaunchKernelEx(&l.cfg, fp8_stage_kernel<__half>, static_cast<const __half*>(a.x), a.ldx, codes, scales, a.M, a.K, words, Mp);
+    return cudaLaunchKernelEx(&l.cfg, fp8_stage_kernel<__nv_bfloat16>, static_cast<const __nv_bfloat16*>(a.x), a.ldx, codes, scales, a.M, a.K, words, Mp);
 }
 
 // ------------------------------------------------------------------------------------------ tensor maps
@@ -178,7 +188,7 @@ extern "C" int slim_fp8_linear(const void* x, int x_type, long long ldx, const v
     a.stream = s;
     if (!slim::fp8_few_takes_x(M)) {
         const slim::Fp8Staging sg = slim::fp8_staging(M, K);
-        SLIM_CUDA_TRY(slim::fp8_stage(a, a.workspace + sg.codes, a.workspace + sg.scales, sg.Mp));
+        SLIM_CUDA_TRY(slim::fp8_stage(a, a.workspace + sg.codes, reinterpret_cast<uint32_t*>(a.workspace + sg.scales), sg.Mp));
         a.x_codes = a.workspace + sg.codes;
         a.x_scales = reinterpret_cast<const uint32_t*>(a.workspace + sg.scales);
         a.Mp = sg.Mp;

@@ -28,8 +28,9 @@ constexpr int kFgStages = 6;
 constexpr int kFgSlot = 2 * 128 * 128;
 constexpr int kFgOffBar = kFgStages * kFgSlot;
 constexpr int kFgSmem = kFgOffBar + 256 + 1024;
-constexpr int kFgColScales = kFgFeat;              // tensor memory: D, then two buffers of 4 + 8 columns of scale words
-constexpr int kFgScaleCols = 16;
+constexpr int kFgColScales = 480;                  // tensor memory: D (twice, where it has at most 224 columns), then two buffers of 4 + 8 columns of
+constexpr int kFgScaleCols = 16;                   // scale words
+constexpr int kFgFeatTwice = 224;
 
 struct FgParams {
     const uint32_t* x_scales;    // [ceil(G / 4)][Mp]
@@ -84,27 +85,26 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     extern __shared__ unsigned char fg_raw[];
     unsigned char* smem = fg_raw + ((1024u - (smem_u32(fg_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem), bars = base + kFgOffBar;
-    auto full = [&](int s) { return bars + 8u * s; };                         // this CTA's slot has landed
-    auto peer = [&](int s) { return bars + 8u * (kFgStages + s); };           // leader's: the other CTA's has
-    auto empty = [&](int s) { return bars + 8u * (2 * kFgStages + s); };
-    auto sf_full = [&](int b) { return bars + 8u * (3 * kFgStages + b); };    // leader's: the scale warps of both CTAs
-    auto sf_empty = [&](int b) { return bars + 8u * (3 * kFgStages + 2 + b); };
-    const uint32_t d_full = bars + 8u * (3 * kFgStages + 4), d_empty = d_full + 8u;      // d_empty: leader's, the output warps of both CTAs
-    static_assert(8 * (3 * kFgStages + 6) <= 240, "room for the barriers");
+    auto full = [&](int s) { return bars + 8u * s; };                         // this CTA's slot has landed; the leader's: and the other CTA's
+    auto empty = [&](int s) { return bars + 8u * (kFgStages + s); };
+    auto sf_full = [&](int b) { return bars + 8u * (2 * kFgStages + b); };    // leader's: the scale warps of both CTAs
+    auto sf_empty = [&](int b) { return bars + 8u * (2 * kFgStages + 2 + b); };
+    auto d_full = [&](int b) { return bars + 8u * (2 * kFgStages + 4 + b); };
+    auto d_empty = [&](int b) { return bars + 8u * (2 * kFgStages + 6 + b); };           // leader's, the output warps of both CTAs
+    static_assert(8 * (2 * kFgStages + 8) <= 240, "room for the barriers");
     volatile int* abort = reinterpret_cast<volatile int*>(smem + kFgOffBar + 240);
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + kFgOffBar + 244);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(tc::uniform(tid >> 5));
     const int rank = static_cast<int>(cluster_ctarank());
     const int pair = static_cast<int>(blockIdx.x >> 1), pairs = static_cast<int>(gridDim.x >> 1);
-    const int G = p.G, feat = p.feat;
+    const int G = p.G, feat = p.feat, bufs = feat <= kFgFeatTwice ? 2 : 1;      // of D
 
     if (tid == 0) {
         *abort = 0;
-        for (int s = 0; s < kFgStages; ++s) { sb::init(full(s), 1); sb::init(peer(s), 1); sb::init(empty(s), 1); }
+        for (int s = 0; s < kFgStages; ++s) { sb::init(full(s), rank == 0 ? 2 : 1); sb::init(empty(s), 1); }
         for (int b = 0; b < 2; ++b) { sb::init(sf_full(b), 8); sb::init(sf_empty(b), 1); }
-        sb::init(d_full, 1);
-        sb::init(d_empty, 16);
+        for (int b = 0; b < 2; ++b) { sb::init(d_full(b), 1); sb::init(d_empty(b), 16); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -139,40 +139,50 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                 }
                 if (g < G) break;
             }
-        } else if (warp == 1) {
-            int words = 0;                             // groups of four blocks begun
-            uint32_t tiles_done = 0;
-            for (int tile = pair; tile < p.tiles; tile += pairs, ++tiles_done) {
-                int g = 0;
-                if (rank == 0 && !tc::warp_wait(d_empty, (tiles_done & 1u) ^ 1u, abort)) break;
-                for (; g < G; ++g, ++issued) {
-                    const int s = issued % kFgStages;
-                    const uint32_t ph = (issued / kFgStages) & 1u;
-                    if (!tc::warp_wait(full(s), ph, abort)) break;
-                    if (rank != 0) {
-                        if (tc::elect()) fg::arrive_cluster(fg::map_to_cta(peer(s), 0));
-                        __syncwarp();
-                        continue;
-                    }
-                    if (!tc::warp_wait(peer(s), ph, abort)) break;
+        } else if (warp == 1 && rank == 0) {
+            // The MMAs of a block take 512 cycles (256 features) and a turn of this loop must not: a wait for a barrier that is ready costs some
+            // 110 cycles, so a slot has one barrier for both CTAs' halves, and the scale words one per four blocks.
+            int words = 0, s = 0;                      // groups of four blocks begun; slot
+            uint32_t ph = 0, phd = 0;
+            int buf = 0;
+            bool ok = true;
+            for (int tile = pair; tile < p.tiles && ok; tile += pairs) {
+                const uint32_t d = tmem + static_cast<uint32_t>(feat * buf);
+                ok = tc::warp_wait(d_empty(buf), phd ^ 1u, abort);
+                for (int g = 0; g < G && ok; ++g, ++issued) {
                     const int b = words & 1;
-                    if ((g & 3) == 0 && !tc::warp_wait(sf_full(b), (words >> 1) & 1u, abort)) break;
+                    if ((g & 3) == 0 && !tc::warp_wait(sf_full(b), (words >> 1) & 1u, abort)) { ok = false; break; }
+                    if (!tc::warp_wait(full(s), ph, abort)) { ok = false; break; }
                     tc::fence_after();
                     const uint64_t a = tc::desc_k128(base + s * kFgSlot), w = tc::desc_k128(base + s * kFgSlot + kFgSlot / 2);
                     const uint32_t idesc = fg::idesc_scaled(kFgTok, feat, g & 3), sa = tmem + kFgColScales + kFgScaleCols * b;
                     const bool last = (g & 3) == 3 || g + 1 == G;
                     if (tc::elect()) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) fg::mma_scaled(tmem, a + 2 * k, w + 2 * k, idesc, sa, sa + 4, g > 0 || k > 0 ? 1u : 0u);
+                        for (int k = 0; k < 4; ++k) fg::mma_scaled(d, a + 2 * k, w + 2 * k, idesc, sa, sa + 4, g > 0 || k > 0 ? 1u : 0u);
                         fg::commit(empty(s));
                         if (last) fg::commit(sf_empty(b));
-                        if (g + 1 == G) fg::commit(d_full);
+                        if (g + 1 == G) fg::commit(d_full(buf));
                     }
                     __syncwarp();
                     if (last) ++words;
+                    if (++s == kFgStages) { s = 0; ph ^= 1u; }
                 }
-                if (g < G) break;
+                if (++buf == bufs) { buf = 0; phd ^= 1u; }
             }
+        } else if (warp == 1) {
+            // tells the leader that this CTA's half of a slot has landed
+            int s = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (int tile = pair; tile < p.tiles && ok; tile += pairs)
+                for (int g = 0; g < G; ++g) {
+                    ok = tc::warp_wait(full(s), ph, abort);
+                    if (!ok) break;
+                    if (tc::elect()) fg::arrive_cluster(fg::map_to_cta(full(s), 0));
+                    __syncwarp();
+                    if (++s == kFgStages) { s = 0; ph ^= 1u; }
+                }
         } else if (warp >= 4) {
             // ---- scale words: this warp's quarter of the lanes, of all of the CTA's tokens and the tile's features
             const int q = warp & 3;
@@ -212,21 +222,24 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kFgRegsMany));
         const int half = (warp - 8) >> 2, q = warp & 3, cols = feat / 2;
         const uint32_t d_t = tmem + static_cast<uint32_t>(cols * half) + (static_cast<uint32_t>(32 * q) << 16);
-        const uint32_t d_empty_leader = fg::map_to_cta(d_empty, 0);
+        const uint32_t d_empty_leader = fg::map_to_cta(d_empty(0), 0);
         uint32_t ph = 0;
-        for (int tile = pair; tile < p.tiles; tile += pairs, ph ^= 1u) {
+        int buf = 0;
+        for (int tile = pair; tile < p.tiles; tile += pairs) {
             const int token = tile % p.tok_tiles * kFgTok + 128 * rank + 32 * q + lane;
             const int n0 = tile / p.tok_tiles * feat + cols * half;
             uint32_t d[8][16];
-            if (!tc::warp_wait(d_full, ph, abort)) break;
+            if (!tc::warp_wait(d_full(buf), ph, abort)) break;
             tc::fence_after();
+            const uint32_t d_b = d_t + static_cast<uint32_t>(feat * buf);
 #pragma unroll
             for (int c = 0; c < 8; ++c)
-                if (16 * c < cols) f8::ld16(d_t + 16 * c, d[c]);
+                if (16 * c < cols) f8::ld16(d_b + 16 * c, d[c]);
             tc::wait_ld();
             tc::fence_before();
             __syncwarp();
-            if (lane == 0) fg::arrive_cluster(d_empty_leader);
+            if (lane == 0) fg::arrive_cluster(d_empty_leader + 8u * buf);
+            if (++buf == bufs) { buf = 0; ph ^= 1u; }
             if (token < p.M) {
                 const size_t at = static_cast<size_t>(token) * p.ldy + n0;
 #pragma unroll
@@ -280,6 +293,19 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
 }
 
 // ------------------------------------------------------------------------------------------ host side
+// Features of a tile: a multiple of 32.  The MMAs of a block take twice as many cycles as there are features, and a block no less than 330 however few
+// (the issuing warp's turn); with one buffer for D, 256 features, a tile waits for the one before it to be read.
+static int fg_features(int tok_tiles, int N, int G, int pairs) {
+    int best = kFgFeat;
+    double least = 1e30;
+    for (int feat = kFgFeat; feat >= 64; feat -= 32) {
+        const long long tiles = static_cast<long long>(tok_tiles) * ((N + feat - 1) / feat), waves = (tiles + pairs - 1) / pairs;
+        const double t = static_cast<double>(waves) * (G * (feat > 165 ? 2.0 * feat : 330.0) + (feat > kFgFeatTwice ? 800.0 : 0.0));
+        if (t < 0.99 * least) { least = t; best = feat; }
+    }
+    return best;
+}
+
 cudaError_t fp8_gemm(const Fp8Args& a) {
     static std::atomic<bool> attr_set[64];    // zero-initialised; set-up is idempotent, so a race repeats it harmlessly
     int dev = 0;
@@ -297,7 +323,7 @@ cudaError_t fp8_gemm(const Fp8Args& a) {
     p.y_type = a.y_type; p.M = a.M; p.N = a.N; p.G = (a.K + f8::kBlock - 1) / f8::kBlock; p.Mp = a.Mp;
     p.tok_tiles = (a.M + kFgTok - 1) / kFgTok;
     const int pairs = device_sm_count() / 2;
-    p.feat = kFgFeat;
+    p.feat = fg_features(p.tok_tiles, a.N, p.G, pairs);
     p.tiles = p.tok_tiles * ((a.N + p.feat - 1) / p.feat);
     CUtensorMap x_map, w_map;
     if (!make_byte_map(&x_map, a.x_codes, a.M, a.K, 128) || !make_byte_map(&w_map, a.codes, a.N, a.K, p.feat / 2)) return cudaErrorUnknown;
