@@ -418,17 +418,18 @@ int slim_gptq_quantize(const void* W, const void* x, const uint8_t* bits_host, d
  * 2^-126; 1 for a block of zeros), code = v / s rounded to nearest even; what is not finite becomes NaN.  s being a power of two, v / s
  * is exact, so the codes are unique.  The last blocks may be ragged.
  *   W fp32, fp16 or bf16 [N][K], row stride ld (a multiple of 8 elements, of 4 for fp32); codes uint8 [N][K]; scales fp32
- *   [ceil(N/128)][ceil(K/128)].  Other scales than the quantizer's serve slim_fp8_linear as well. */
+ *   [ceil(N/128)][ceil(K/128)]. */
 int slim_fp8_quantize(const void* W, int type, long long ld, void* codes, float* scales, int N, int K, void* stream);
 
 /* Host-only: workspace of slim_fp8_linear for these shapes: the header (and flags) of slim_workspace_bytes, then, beyond 32 tokens, the codes
  * and scales of x.  One of the larger size may be shared with the other linear layers' calls on one stream (initialised by slim_workspace_init). */
 int slim_fp8_workspace_bytes(int M, int N, int K, size_t* out_bytes);
 
-/* y[m][n] = sum_g sx[m][g] * scales[n/128][g] * sum_{k in block g} e4m3(x)[m][k] * codes[n][k]: the inner sums by the tensor
- * cores (fp32 accumulator), the outer one in fp32; one rounding to y.  Any M >= 1 (one token and thousands alike) and N; K a multiple of 16.
+/* y[m][n] = sum_g sx[m][g] * scales[n/128][g] * sum_{k in block g} e4m3(x)[m][k] * codes[n][k], by the tensor
+ * cores (fp32 accumulator; the scales are applied inside); one rounding to y.  Any M >= 1 (one token and thousands alike) and N; K a multiple of 16.
  *   x fp16 or bf16 [M][K], row stride ldx (a multiple of 8 elements); y of x's type or fp32 [M][N], row stride ldy.
- * NaN or infinity in x gives NaN in that token's row of y alone, in the codes (0x7f, 0xff) or scales in the outputs of their rows of W.
+ * scales: powers of two from 2^-126 to 2^127, as the quantizer gives them (the tensor cores take their exponents; of any other value
+ * only the exponent counts).  NaN or infinity in x gives NaN in that token's row of y alone, NaN codes (0x7f, 0xff) in the outputs of their rows of W.
  * The gradient of x for a frozen W, dx = dy * W, is the same call on the transposed layer: codes^T [K][N] and scales^T, with x = dy.
  * Deterministic.  A wait that gives up is reported by slim_workspace_status. */
 #define SLIM_FP8_MAX_K 262144

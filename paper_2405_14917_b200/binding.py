@@ -709,7 +709,10 @@ class Fp8Linear:
     prepare_input_grad lays out once (as many bytes again; N a multiple of 16)."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        """codes and scales of fp8_quantize, or of a checkpoint whose scales are powers of two (looked at here, once: a synchronisation)."""
         _dev(codes, torch.float8_e4m3fn, "codes"), _dev(scales, torch.float32, "scales")
+        if not bool(((scales.view(torch.int32) & 0x7fffff) == 0).all() & (scales > 0).all() & torch.isfinite(scales).all()):
+            raise ValueError("scales must be powers of two")
         if codes.dim() != 2 or tuple(scales.shape) != ((codes.shape[0] + 127) // 128, (codes.shape[1] + 127) // 128):
             raise ValueError("codes must be [N][K] and scales [ceil(N/128)][ceil(K/128)]")
         self.codes, self.scales = codes, scales

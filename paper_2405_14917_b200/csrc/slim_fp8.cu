@@ -1,7 +1,7 @@
 // slim_fp8_quantize, slim_fp8_linear: a linear layer in 8-bit floats (e4m3), the group-wise layer's counterpart for the weights that
 // one to four bits do not do: W in blocks of 128 x 128 with one fp32 scale each, x quantised inside the call in blocks of 128 columns of a token,
 //     y[m][n] = sum_g sx[m][g] * sw[n / 128][g] * sum_{k in block g} xq[m][k] * wq[n][k]
-// with the inner sums on the tensor cores (tcgen05, e4m3 in, fp32 accumulator) and the outer one in fp32 registers.
+// on the tensor cores (tcgen05, e4m3 in, fp32 accumulator), which apply the scales too: they are powers of two.
 // This file: the two quantizers, which kernel a call goes to, and the entry points.
 #include "slim_fp8.cuh"
 
@@ -12,47 +12,82 @@ namespace slim {
 // ------------------------------------------------------------------------------------------ W
 // A block of 256 threads per 128 x 128 block of W; thread (r, c): row r + 16 i, columns 8c .. 8c + 7.  Bound: HBM, one read and
 // one write; the block stays in registers between its maximum and its codes.
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* f) { f8::unpack8<T>(__ldcs(reinterpret_cast<const uint4*>(p)), f); }
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* f) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
+// Eight elements of W as they lie in memory, their largest magnitude (as fp32 bits; anything from infinity's on is not finite), their codes.
+template <typename T> struct W8 {
+    uint4 v;
+    __device__ __forceinline__ void load(const T* p) { v = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void unpack(float* f) const { f8::Half16<T>::unpack(v, f); }
+    // over several: halves of 16 bits, joined at the end
+    __device__ __forceinline__ void top(uint32_t& m) const { m = __vmaxu2(m, f8::top2(v)); }
+    static __device__ __forceinline__ uint32_t join(uint32_t m) {
+        m = max(m & 0xffffu, m >> 16);
+        return __float_as_uint(f8::Half16<T>::one(m));
+    }
+};
+template <> struct W8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) { a = __ldcs(reinterpret_cast<const float4*>(p)); b = __ldcs(reinterpret_cast<const float4*>(p) + 1); }
+    __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void unpack(float* f) const { f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w; }
+    __device__ __forceinline__ void top(uint32_t& m) const {
+        float f[8];
+        unpack(f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(f[e]) & 0x7fffffffu);
+    }
+    static __device__ __forceinline__ uint32_t join(uint32_t m) { return m; }
+};
 template <typename T>
 __global__ void __launch_bounds__(256) fp8_quantize_kernel(const T* __restrict__ W, long long ld, uint8_t* __restrict__ codes,
                                                            float* __restrict__ scales, int N, int K) {
     __shared__ uint32_t s_max[8];
     const int tid = threadIdx.x, c = tid & 15, r = tid >> 4;
     const int n0 = blockIdx.y * f8::kBlock, k = blockIdx.x * f8::kBlock + 8 * c;
-    float f[8][8];
+    W8<T> v[8];
     uint32_t mx = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int n = n0 + r + 16 * i;
-        if (n < N && k < K) load8(W + static_cast<size_t>(n) * ld + k, f[i]);
-        else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[i][e] = 0.f;
-        }
+        if (n < N && k < K) v[i].load(W + static_cast<size_t>(n) * ld + k);
+        else v[i].zero();
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mx = max(mx, f8::magnitude(f[i][e]));
-    mx = __reduce_max_sync(0xffffffffu, mx);
+    for (int i = 0; i < 8; ++i) v[i].top(mx);
+    mx = __reduce_max_sync(0xffffffffu, W8<T>::join(mx));
     if ((tid & 31) == 0) s_max[tid >> 5] = mx;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 8; ++w) mx = max(mx, s_max[w]);
+    const bool finite = mx < 0x7f800000u;
+    if (!finite) {                                     // the whole block of threads: once more, of what is finite
+        mx = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float f[8];
+            v[i].unpack(f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mx = max(mx, f8::magnitude(f[e]));
+        }
+        mx = __reduce_max_sync(0xffffffffu, mx);
+        __syncthreads();
+        if ((tid & 31) == 0) s_max[tid >> 5] = mx;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 8; ++w) mx = max(mx, s_max[w]);
+    }
     const uint32_t sb = f8::scale_bits(mx);
     const float inv = f8::inverse_scale(sb);
     if (tid == 0) scales[static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x] = __uint_as_float(sb);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int n = n0 + r + 16 * i;
-        if (n < N && k < K)
-            *reinterpret_cast<uint2*>(codes + static_cast<size_t>(n) * K + k) = make_uint2(f8::codes4(f[i], inv), f8::codes4(f[i] + 4, inv));
+        if (n < N && k < K) {
+            float f[8];
+            v[i].unpack(f);
+            *reinterpret_cast<uint2*>(codes + static_cast<size_t>(n) * K + k) =
+                finite ? make_uint2(f8::codes4<false>(f, inv), f8::codes4<false>(f + 4, inv)) : make_uint2(f8::codes4<true>(f, inv), f8::codes4<true>(f + 4, inv));
+        }
     }
 }
 
@@ -78,17 +113,10 @@ __global__ void __launch_bounds__(256) fp8_stage_kernel(const T* __restrict__ x,
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int k = (4 * j + i) * f8::kBlock + 8 * c;
-        float f[8];
-        f8::unpack8<T>(v[i], f);
-        uint32_t mx = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mx = max(mx, f8::magnitude(f[e]));
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const uint32_t sb = f8::scale_bits(mx);
-        const float inv = f8::inverse_scale(sb);
-        if (m < M && k < K) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(m) * K + k) = make_uint2(f8::codes4(f, inv), f8::codes4(f + 4, inv));
-        word |= (sb >> 23) << (8 * i);
+        uint32_t e;
+        const uint2 q = f8::quantise8<T>(v[i], e);
+        if (m < M && k < K) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(m) * K + k) = q;
+        word |= e << (8 * i);
     }
     if (c == 0 && m < M) scales[static_cast<size_t>(j) * Mp + m] = word;
 }

@@ -25,15 +25,18 @@ __device__ __forceinline__ uint32_t scale_bits(uint32_t amax) {
 // 1 / s for s of scale_bits (2^-126 .. 2^119): exact.
 __device__ __forceinline__ float inverse_scale(uint32_t bits) { return __uint_as_float((254u << 23) - bits); }
 
-// Four codes of v * inv; what is not finite becomes NaN (e4m3 has no infinity, and 448 would pass for a value).
+// Four codes of v * inv.  NaN gives NaN (0x7f or 0xff); `checked` makes NaN of infinities too (e4m3 has none, and 448 would pass for a value).
+template <bool checked>
 __device__ __forceinline__ uint32_t codes4(const float* v, float inv) {
     uint16_t lo, hi;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(v[1] * inv), "f"(v[0] * inv));
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(v[3] * inv), "f"(v[2] * inv));
     uint32_t r = static_cast<uint32_t>(lo) | static_cast<uint32_t>(hi) << 16;
+    if (checked) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (!(fabsf(v[i]) <= 3.402823466e38f)) r |= 0x7fu << (8 * i);
+        for (int i = 0; i < 4; ++i)
+            if (!(fabsf(v[i]) <= 3.402823466e38f)) r |= 0x7fu << (8 * i);
+    }
     return r;
 }
 // Magnitude for the block's maximum: what is not finite does not count.
@@ -42,20 +45,56 @@ __device__ __forceinline__ uint32_t magnitude(float v) {
     return m < 0x7f800000u ? m : 0u;
 }
 
-// Eight elements of a row as floats: 16 bytes of a 16-bit type, 32 of fp32.
-template <typename T> __device__ __forceinline__ void unpack8(const uint4& v, float* f);
-template <> __device__ __forceinline__ void unpack8<__half>(const uint4& v, float* f) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// Eight elements of a 16-bit type as floats, the bits of its infinity, and one from its bits.
+template <typename T> struct Half16;
+template <> struct Half16<__half> {
+    static constexpr uint32_t INF = 0x7c00u;
+    static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        f[2 * i] = t.x; f[2 * i + 1] = t.y;
+        for (int i = 0; i < 4; ++i) {
+            const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            f[2 * i] = t.x; f[2 * i + 1] = t.y;
+        }
     }
-}
-template <> __device__ __forceinline__ void unpack8<__nv_bfloat16>(const uint4& v, float* f) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    static __device__ __forceinline__ float one(uint32_t bits) { return __half2float(__ushort_as_half(static_cast<unsigned short>(bits))); }
+};
+template <> struct Half16<__nv_bfloat16> {
+    static constexpr uint32_t INF = 0x7f80u;
+    static __device__ __forceinline__ void unpack(const uint4& v, float* f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+    static __device__ __forceinline__ float one(uint32_t bits) { return __uint_as_float(bits << 16); }
+};
+// Largest magnitudes of eight elements, as bits, in two halves: without their signs the bits are in the order of the values.
+__device__ __forceinline__ uint32_t top2(const uint4& v) {
+    return __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+}
+// The block of 128 that half a warp holds, eight elements a lane: this lane's codes, and the scale's exponent.  All lanes of the warp take part.
+template <typename T>
+__device__ __forceinline__ uint2 quantise8(const uint4& v, uint32_t& exponent) {
+    uint32_t m = top2(v);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
+    m = max(m & 0xffffu, m >> 16);
+    float f[8];
+    Half16<T>::unpack(v, f);
+    const bool finite = m < Half16<T>::INF;
+    uint32_t bits = __float_as_uint(Half16<T>::one(m));
+    if (__any_sync(0xffffffffu, !finite)) {
+        uint32_t mx = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mx = max(mx, magnitude(f[e]));
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        bits = mx;
+    }
+    const uint32_t sb = scale_bits(bits);
+    const float inv = inverse_scale(sb);
+    exponent = sb >> 23;
+    return finite ? make_uint2(codes4<false>(f, inv), codes4<false>(f + 4, inv)) : make_uint2(codes4<true>(f, inv), codes4<true>(f + 4, inv));
 }
 
 // y element: `type` is SLIM_F32, SLIM_F16 or SLIM_BF16; one rounding of the fp32 sum.
@@ -65,17 +104,6 @@ __device__ __forceinline__ void store_y(void* y, int type, size_t at, float v) {
     else static_cast<__nv_bfloat16*>(y)[at] = __float2bfloat16_rn(v);
 }
 
-// D[tmem] (+)= A[smem] B[smem]^T, e4m3 in, fp32 accumulate.
-__device__ __forceinline__ void mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
-}
-// Instruction descriptor: e4m3 operands, both K-major, fp32 accumulator, m x n.
-__host__ __device__ constexpr uint32_t idesc(int m, int n) {
-    return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
-}
 // 32 lanes x 16 columns of 32 bits
 __device__ __forceinline__ void ld16(uint32_t taddr, uint32_t* v) {
     asm volatile(

@@ -1,42 +1,45 @@
 // The 8-bit linear layer for few tokens: W is the M dimension of the MMA (128 rows per CTA), up to 128 tokens its N dimension.
 //
 // Bound: HBM, the codes of W (one byte per weight).  A tile of 128 rows is cut along K over the CTAs of a cluster, so that
-// narrow layers too have about two CTAs per SM and everything a CTA reads is in flight at once: TMA brings 128 x 128 bytes per block of
-// 128 columns into a ring of 128-byte-swizzled slots, four K = 32 MMAs per block leave its sums in one of two buffers of tensor memory,
-// and four warps take them from there into fp32 registers under the block's scale.  The CTAs of a cluster then add their sums
-// through distributed shared memory, every CTA a share of the tokens, in rank order: no workspace, no second kernel, one result.
+// narrow layers too have about two CTAs per SM and most of what a CTA reads is in flight at once: TMA brings 128 x 128 bytes per block of
+// 128 columns into a ring of 128-byte-swizzled slots, and four K = 32 MMAs per block (block-scaled, E8M0: see slim_fp8_gemm.cu) add it to D in
+// tensor memory.  Both operands' scales of a block are one byte per row, written to tensor memory by tcgen05.st (row r's at lane r % 32 of column
+// r / 32, the same in all lane quarters) into a buffer per slot.  At the end the CTAs of a cluster add their sums through
+// distributed shared memory, every CTA a share of the tokens, in rank order: no workspace, no second kernel, one result.
 //
-// Up to 32 tokens x is quantised here (kTakesX), by four warps ahead of the MMAs, from x itself: every CTA does it for its part of K,
+// Up to 32 tokens x is quantised here (TAKES_X), by four warps ahead of the MMAs, from x itself: every CTA does it for its part of K,
 // which costs L2 reads of 2 T bytes per 128 bytes of W and saves the launch of the quantizer.  Beyond, the codes come
 // by TMA from the workspace (slim_fp8.cu).
 //
-// Warps: 0 loads of W (and of staged x); 1 MMAs, tensor memory; 2, 3, 8, 9 quantisation of x, or the scales of staged x;
-// 4 to 7 sums (tensor-memory lanes 32 (w % 4) on).  Every wait is bounded and reports through the workspace status word.
+// Warps: 0 loads of W (and of staged x); 1 MMAs, tensor memory; 4 to 7 scales, then the output (tensor-memory lanes 32 (w % 4) on); 2, 3, 8, 9
+// quantisation of x.  Every wait is bounded and reports through the workspace status word.
 #include "slim_fp8.cuh"
 
 #include <atomic>
 
 namespace slim {
 
-constexpr int kFewThreads = 320;
 constexpr int kFewXWarps = 4;
 constexpr int kFewMaxCluster = 8;
 
 template <int T> struct FewCfg {
     static constexpr bool TAKES_X = T <= 32;
-    static constexpr int PER_SM = T <= 64 ? 2 : 1;
+    static constexpr int THREADS = TAKES_X ? 320 : 256;
     static constexpr int W_BYTES = 128 * 128, X_BYTES = T * 128;
-    static constexpr int STAGES = T <= 16 ? 5 : T <= 32 ? 5 : T <= 64 ? 4 : 6;
-    static constexpr int TMEM = 2 * T < 32 ? 32 : 2 * T;
-    static constexpr int OFF_SX = STAGES * (W_BYTES + X_BYTES);           // [STAGES][T] fp32
-    static constexpr int OFF_BAR = OFF_SX + STAGES * T * 4;
+    static constexpr int STAGES = T <= 32 ? 5 : T <= 64 ? 4 : 3;
+    static constexpr int AHEAD = T <= 16 ? 4 : 2;                         // blocks of x on their way to the quantising warps
+    static constexpr int COL_SF = T;                                      // tensor memory: D, then per slot 4 columns of W's scales and T / 32 of x's
+    static constexpr int TMEM_USED = T + 8 * STAGES;
+    static constexpr int TMEM = TMEM_USED <= 64 ? 64 : TMEM_USED <= 128 ? 128 : 256;
+    static constexpr int OFF_SX = STAGES * (W_BYTES + X_BYTES);           // TAKES_X: [STAGES][T] scale exponents
+    static constexpr int OFF_BAR = OFF_SX + STAGES * T;
     static constexpr int SMEM = OFF_BAR + 256 + 1024;                     // + alignment of the slots
 };
 
 struct FewParams {
     const void* x;
     long long ldx;
-    const uint8_t* x_scales;     // staged: exponents, byte g % 4 of word [g / 4][token]
+    const uint32_t* x_scales;    // staged: exponents of four blocks in a word, [ceil(G / 4)][Mp]
     const float* scales;
     void* y;
     long long ldy;
@@ -44,21 +47,29 @@ struct FewParams {
     int y_type, M, N, K, G, Mp, ranks;
 };
 
+namespace few {
+__device__ __forceinline__ void mma_scaled(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+}
+}  // namespace few
+
 template <int T, typename X>
-__global__ void __launch_bounds__(kFewThreads, FewCfg<T>::PER_SM)
+__global__ void __launch_bounds__(FewCfg<T>::THREADS, 2)
 fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map, const FewParams p) {
     using C = FewCfg<T>;
     extern __shared__ unsigned char few_raw[];
     unsigned char* smem = few_raw + ((1024u - (smem_u32(few_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(smem);
-    const uint32_t s_x = base + C::STAGES * C::W_BYTES, s_sx = base + C::OFF_SX, bars = base + C::OFF_BAR;
-    auto w_full = [&](int s) { return bars + 8u * s; };
-    auto w_empty = [&](int s) { return bars + 8u * (C::STAGES + s); };
-    auto x_full = [&](int s) { return bars + 8u * (2 * C::STAGES + s); };
-    auto x_empty = [&](int s) { return bars + 8u * (3 * C::STAGES + s); };
-    auto d_full = [&](int b) { return bars + 8u * (4 * C::STAGES + b); };
-    auto d_empty = [&](int b) { return bars + 8u * (4 * C::STAGES + 2 + b); };
-    static_assert(8 * (4 * C::STAGES + 4) <= 240, "room for the barriers");
+    const uint32_t s_x = base + C::STAGES * C::W_BYTES, bars = base + C::OFF_BAR;
+    auto w_full = [&](int s) { return bars + 8u * s; };                   // W's block, and staged x's, has landed
+    auto x_full = [&](int s) { return bars + 8u * (C::STAGES + s); };     // TAKES_X: x's codes and exponents are written
+    auto sf_full = [&](int s) { return bars + 8u * (2 * C::STAGES + s); };
+    auto empty = [&](int s) { return bars + 8u * (3 * C::STAGES + s); };
+    const uint32_t d_full = bars + 8u * (4 * C::STAGES);
+    static_assert(8 * (4 * C::STAGES + 1) <= 240, "room for the barriers");
     volatile int* abort = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 240);
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + C::OFF_BAR + 244);
 
@@ -68,17 +79,17 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
     const int nb = tile % row_tiles, n0 = 128 * nb, m0 = tile / row_tiles * T;
     const int tokens = min(T, p.M - m0);
     const int g0 = static_cast<int>(static_cast<long long>(p.G) * rank / p.ranks), g1 = static_cast<int>(static_cast<long long>(p.G) * (rank + 1) / p.ranks);
-    const int steps = g1 - g0;
+    const int steps = g1 - g0;                         // at least 1: there are no more ranks than blocks
 
     if (tid == 0) {
         *abort = 0;
         for (int s = 0; s < C::STAGES; ++s) {
             sb::init(w_full(s), 1);
-            sb::init(w_empty(s), 1);
-            sb::init(x_full(s), C::TAKES_X ? kFewXWarps : 2);      // quantising warps, or the codes' TMA and the warp with their scales
-            sb::init(x_empty(s), 1 + 4);                           // MMAs, and the warps that read the scales
+            sb::init(x_full(s), kFewXWarps);
+            sb::init(sf_full(s), 4);
+            sb::init(empty(s), 1);
         }
-        for (int b = 0; b < 2; ++b) { sb::init(d_full(b), 1); sb::init(d_empty(b), 4); }
+        sb::init(d_full, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -86,9 +97,9 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
         tc::relinquish();
     }
     if (C::TAKES_X) {                                  // tokens past the last stay zero
-        for (int i = tid; i < C::STAGES * C::X_BYTES / 16; i += kFewThreads)
+        for (int i = tid; i < C::STAGES * C::X_BYTES / 16; i += C::THREADS)
             *reinterpret_cast<uint4*>(smem + C::STAGES * C::W_BYTES + 16 * i) = make_uint4(0, 0, 0, 0);
-        for (int i = tid; i < C::STAGES * T; i += kFewThreads) *reinterpret_cast<float*>(smem + C::OFF_SX + 4 * i) = 0.f;
+        for (int i = tid; i < C::STAGES * T; i += C::THREADS) smem[C::OFF_SX + i] = 127;
         tc::fence_proxy_async();
     }
     tc::fence_before();
@@ -98,174 +109,174 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
     pdl_launch_dependents();
     pdl_wait();
 
-    float acc[T];                                      // this thread's row, all tokens (warps 4 to 7)
     if (warp == 0) {
         // ---- W, and the codes of staged x
+        int s = 0;
+        uint32_t ph = 0;
         for (int i = 0; i < steps; ++i) {
-            const int s = i % C::STAGES;
-            const uint32_t ph = (i / C::STAGES) & 1u;
-            if (!tc::warp_wait(w_empty(s), ph ^ 1u, abort)) break;
-            if (!C::TAKES_X && !tc::warp_wait(x_empty(s), ph ^ 1u, abort)) break;
+            if (!tc::warp_wait(empty(s), ph ^ 1u, abort)) break;
             if (tc::elect()) {
-                sb::expect_tx(w_full(s), C::W_BYTES);
+                sb::expect_tx(w_full(s), C::TAKES_X ? C::W_BYTES : C::W_BYTES + C::X_BYTES);
                 tc::tma_load_2d(base + s * C::W_BYTES, &w_map, 128 * (g0 + i), n0, w_full(s));
-                if (!C::TAKES_X) {
-                    sb::expect_tx(x_full(s), C::X_BYTES);
-                    tc::tma_load_2d(s_x + s * C::X_BYTES, &x_map, 128 * (g0 + i), m0, x_full(s));
-                }
+                if (!C::TAKES_X) tc::tma_load_2d(s_x + s * C::X_BYTES, &x_map, 128 * (g0 + i), m0, w_full(s));
             }
             __syncwarp();
+            if (++s == C::STAGES) { s = 0; ph ^= 1u; }
         }
     } else if (warp == 1) {
         // ---- MMAs
+        // e4m3 operands, both K-major, E8M0 scales (the lowest byte of their words), 128 x T
+        constexpr uint32_t idesc = (static_cast<uint32_t>(T >> 3) << 17) | (1u << 23) | (1u << 27);
+        int s = 0;
+        uint32_t ph = 0;
         for (int i = 0; i < steps; ++i) {
-            const int s = i % C::STAGES, b = i & 1;
-            const uint32_t ph = (i / C::STAGES) & 1u;
-            if (!tc::warp_wait(d_empty(b), ((i >> 1) & 1u) ^ 1u, abort)) break;
-            if (!tc::warp_wait(x_full(s), ph, abort)) break;
+            if (!tc::warp_wait(sf_full(s), ph, abort)) break;             // behind x_full, where x is quantised here
             if (!tc::warp_wait(w_full(s), ph, abort)) break;
             tc::fence_after();
             const uint64_t a = tc::desc_k128(base + s * C::W_BYTES), x = tc::desc_k128(s_x + s * C::X_BYTES);
+            const uint32_t sf = tmem + C::COL_SF + 8u * s;
             if (tc::elect()) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) f8::mma_ss(tmem + b * T, a + 2 * k, x + 2 * k, f8::idesc(128, T), k > 0 ? 1u : 0u);
-                tc::commit(w_empty(s));
-                tc::commit(x_empty(s));
-                tc::commit(d_full(b));
+                for (int k = 0; k < 4; ++k) few::mma_scaled(tmem, a + 2 * k, x + 2 * k, idesc, sf, sf + 4, i > 0 || k > 0 ? 1u : 0u);
+                tc::commit(empty(s));
+                if (i + 1 == steps) tc::commit(d_full);
             }
             __syncwarp();
+            if (++s == C::STAGES) { s = 0; ph ^= 1u; }
         }
-    } else if (warp < 4 || warp >= 8) {
-        const int xw = warp < 4 ? warp - 2 : warp - 6;
-        if (C::TAKES_X) {
-            // ---- x into codes: half a warp per token and block, two tokens of a warp at a time
-            constexpr int PAIRS = T / 2 / kFewXWarps;               // pairs of tokens of a warp
-            const int half = lane >> 4, c = lane & 15;
-            const X* x = static_cast<const X*>(p.x);
-            uint4 v[PAIRS];
-            auto fetch = [&](int i) {
+    } else if (warp >= 4 && warp < 8) {
+        // ---- scales: this warp's quarter of the lanes, of the 128 rows (one scale) and of all tokens
+        const uint32_t sf_t = tmem + C::COL_SF + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
+        const float* sw = p.scales + static_cast<size_t>(nb) * p.G + g0;
+        uint32_t w_now = 0, w_next = lane < steps ? __float_as_uint(__ldg(sw + lane)) : 0u;      // a lane holds one of 32 blocks'
+        constexpr int XC = (T + 31) / 32;
+        uint32_t x_now[XC], x_next[XC];
+        auto x_words = [&](int g, uint32_t* v) {
 #pragma unroll
-                for (int u = 0; u < PAIRS; ++u) {
-                    const int t = 2 * (xw + kFewXWarps * u) + half, k = 128 * (g0 + i) + 8 * c;
-                    v[u] = t < tokens && k < p.K ? __ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(m0 + t) * p.ldx + k)) : make_uint4(0, 0, 0, 0);
+            for (int c = 0; c < XC; ++c) v[c] = g < g1 ? __ldcg(p.x_scales + static_cast<size_t>(g >> 2) * p.Mp + min(m0 + 32 * c + lane, p.Mp - 1)) : 0u;
+        };
+        if (!C::TAKES_X) x_words(g0, x_next);
+        int s = 0;
+        uint32_t ph = 0;
+        for (int i = 0; i < steps; ++i) {
+            if ((i & 31) == 0) {
+                w_now = w_next;
+                w_next = i + 32 + lane < steps ? __float_as_uint(__ldg(sw + i + 32 + lane)) : 0u;
+            }
+            const uint32_t w = __shfl_sync(0xffffffffu, w_now, i & 31) >> 23 & 0xffu;
+            uint32_t v[8] = {w, w, w, w, 0, 0, 0, 0};
+            if (C::TAKES_X) {
+                if (!tc::warp_wait(x_full(s), ph, abort)) break;
+                tc::fence_after();
+                v[4] = lane < T ? smem[C::OFF_SX + s * T + lane] : 127;
+            } else {
+                const int g = g0 + i;
+                if (i == 0 || (g & 3) == 0) {
+#pragma unroll
+                    for (int c = 0; c < XC; ++c) x_now[c] = x_next[c];
+                    x_words((g & ~3) + 4, x_next);
                 }
-            };
-            if (steps > 0) fetch(0);
-            for (int i = 0; i < steps; ++i) {
-                const int s = i % C::STAGES;
-                const uint32_t ph = (i / C::STAGES) & 1u;
-                if (!tc::warp_wait(x_empty(s), ph ^ 1u, abort)) break;
-                uint4 now[PAIRS];
+                if (!tc::warp_wait(empty(s), ph ^ 1u, abort)) break;
+                tc::fence_after();
 #pragma unroll
-                for (int u = 0; u < PAIRS; ++u) now[u] = v[u];
-                if (i + 1 < steps) fetch(i + 1);
+                for (int c = 0; c < XC; ++c) v[4 + c] = x_now[c] >> (8 * (g & 3)) & 0xffu;
+            }
+            tc::st8(sf_t + 8u * s, v);
+            tc::wait_st();
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) sb::arrive(sf_full(s));
+            if (++s == C::STAGES) { s = 0; ph ^= 1u; }
+        }
+    } else if (C::TAKES_X) {
+        // ---- x into codes: half a warp per token and block, two tokens of a warp at a time
+        const int xw = warp < 4 ? warp - 2 : warp - 6;
+        constexpr int PAIRS = T / 2 / kFewXWarps;                         // pairs of tokens of a warp
+        const int half = lane >> 4, c = lane & 15;
+        const X* x = static_cast<const X*>(p.x);
+        uint4 v[C::AHEAD][PAIRS];
+        auto fetch = [&](int i, uint4* o) {
+#pragma unroll
+            for (int u = 0; u < PAIRS; ++u) {
+                const int t = 2 * (xw + kFewXWarps * u) + half, k = 128 * (g0 + i) + 8 * c;
+                o[u] = i < steps && t < tokens && k < p.K ? __ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(m0 + t) * p.ldx + k)) : make_uint4(0, 0, 0, 0);
+            }
+        };
+#pragma unroll
+        for (int a = 0; a < C::AHEAD; ++a) fetch(a, v[a]);
+        int s = 0;
+        uint32_t ph = 0;
+        bool ok = true;
+        for (int i0 = 0; i0 < steps && ok; i0 += C::AHEAD) {
+#pragma unroll
+            for (int a = 0; a < C::AHEAD; ++a) {
+                const int i = i0 + a;
+                if (i >= steps) break;
+                ok = tc::warp_wait(empty(s), ph ^ 1u, abort);
+                if (!ok) break;
 #pragma unroll
                 for (int u = 0; u < PAIRS; ++u) {
                     const int t = 2 * (xw + kFewXWarps * u) + half;
                     if (2 * (xw + kFewXWarps * u) >= tokens) continue;
-                    float f[8];
-                    f8::unpack8<X>(now[u], f);
-                    uint32_t mx = 0;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) mx = max(mx, f8::magnitude(f[e]));
-#pragma unroll
-                    for (int o = 8; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                    const uint32_t sbits = f8::scale_bits(mx);
-                    const float inv = f8::inverse_scale(sbits);
+                    uint32_t e;
+                    const uint2 codes = f8::quantise8<X>(v[a][u], e);
                     // row t of a swizzled tile: its 16-byte chunks stand at chunk ^ (t & 7)
                     const uint32_t at = s_x + s * C::X_BYTES + t * 128 + ((((c >> 1) ^ (t & 7)) << 4) | ((c & 1) << 3));
-                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(f8::codes4(f, inv)), "r"(f8::codes4(f + 4, inv)) : "memory");
-                    if (c == 0) *reinterpret_cast<float*>(smem + C::OFF_SX + 4 * (s * T + t)) = __uint_as_float(sbits);
+                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(codes.x), "r"(codes.y) : "memory");
+                    if (c == 0) smem[C::OFF_SX + s * T + t] = static_cast<uint8_t>(e);
                 }
+                fetch(i + C::AHEAD, v[a]);
                 tc::fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) sb::arrive(x_full(s));
+                if (++s == C::STAGES) { s = 0; ph ^= 1u; }
             }
-        } else if (xw == 0) {
-            // ---- the scales of staged x
-            for (int i = 0; i < steps; ++i) {
-                const int s = i % C::STAGES;
-                const uint32_t ph = (i / C::STAGES) & 1u;
-                if (!tc::warp_wait(x_empty(s), ph ^ 1u, abort)) break;
-#pragma unroll
-                for (int t = lane; t < T; t += 32)
-                    *reinterpret_cast<float*>(smem + C::OFF_SX + 4 * (s * T + t)) = t < tokens ? __uint_as_float(static_cast<uint32_t>(__ldcg(p.x_scales + (static_cast<size_t>((g0 + i) >> 2) * p.Mp + m0 + t) * 4 + ((g0 + i) & 3))) << 23) : 0.f;
-                __syncwarp();
-                if (lane == 0) sb::arrive(x_full(s));
-            }
-        }
-    } else {
-        // ---- sums: D of every block under its scales
-#pragma unroll
-        for (int t = 0; t < T; ++t) acc[t] = 0.f;
-        const float* sw = p.scales + static_cast<size_t>(nb) * p.G + g0;
-        float w_next = steps > 0 ? __ldg(sw) : 0.f;
-        for (int i = 0; i < steps; ++i) {
-            const int s = i % C::STAGES, b = i & 1;
-            const float w = w_next;
-            if (i + 1 < steps) w_next = __ldg(sw + i + 1);
-            // the scales were written by other warps, ahead of the barrier that the MMAs waited for: this warp waits for it too
-            if (!tc::warp_wait(x_full(s), (i / C::STAGES) & 1u, abort)) break;
-            if (!tc::warp_wait(d_full(b), (i >> 1) & 1u, abort)) break;
-            tc::fence_after();
-            const uint32_t d_t = tmem + b * T + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
-#pragma unroll
-            for (int t0 = 0; t0 < T; t0 += 16) {
-                uint32_t d[16];
-                f8::ld16(d_t + t0, d);
-                tc::wait_ld();
-#pragma unroll
-                for (int t = 0; t < 16; t += 4) {
-                    const float4 sx = *reinterpret_cast<const float4*>(smem + C::OFF_SX + 4 * (s * T + t0 + t));
-                    acc[t0 + t] = fmaf(__uint_as_float(d[t]), w * sx.x, acc[t0 + t]);
-                    acc[t0 + t + 1] = fmaf(__uint_as_float(d[t + 1]), w * sx.y, acc[t0 + t + 1]);
-                    acc[t0 + t + 2] = fmaf(__uint_as_float(d[t + 2]), w * sx.z, acc[t0 + t + 2]);
-                    acc[t0 + t + 3] = fmaf(__uint_as_float(d[t + 3]), w * sx.w, acc[t0 + t + 3]);
-                }
-            }
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) { sb::arrive(d_empty(b)); sb::arrive(x_empty(s)); }
         }
     }
 
-    // ---- everything in flight has landed, also after a wait that gave up; then the ring holds the sums of the cluster
-    if (warp == 0)
-        for (int i = max(0, steps - C::STAGES); i < steps && *abort != 0; ++i) {
-            if (tc::elect()) {
-                f8::drain(w_full(i % C::STAGES), (i / C::STAGES) & 1u);
-                if (!C::TAKES_X) f8::drain(x_full(i % C::STAGES), (i / C::STAGES) & 1u);
-            }
+    // ---- D is complete; after a wait that gave up, what is in flight has landed before the shared memory is used again
+    bool done = true;
+    if (warp >= 4 && warp < 8) done = tc::warp_wait(d_full, 0, abort);
+    if (warp == 0 && *abort != 0)
+        for (int s = 0; s < C::STAGES; ++s) {
+            if (tc::elect()) { f8::drain(w_full(s), 0); f8::drain(w_full(s), 1); }
             __syncwarp();
         }
-    if (warp == 1 && *abort != 0) {
-        for (int i = max(0, steps - 2); i < steps; ++i) {
-            if (tc::elect()) f8::drain(d_full(i & 1), (i >> 1) & 1u);
+    if (warp == 1 && *abort != 0)
+        for (int s = 0; s < C::STAGES; ++s) {
+            if (tc::elect()) { f8::drain(empty(s), 0); f8::drain(empty(s), 1); }
             __syncwarp();
         }
-    }
-    tc::fence_before();
+    (void)done;
     __syncthreads();
     tc::fence_after();
-    if (warp == 1) tc::dealloc(tmem, C::TMEM);
     const int row = 32 * (warp & 3) + lane;            // warps 4 to 7
     const bool sums = warp >= 4 && warp < 8;
-    if (p.ranks == 1) {
-        if (sums && n0 + row < p.N) {
+    const uint32_t d_t = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
+    float* part = reinterpret_cast<float*>(smem);      // [T][128], in the ring
+    if (sums) {
+#pragma unroll 1
+        for (int t0 = 0; t0 < tokens; t0 += 16) {
+            uint32_t d[16];
+            f8::ld16(d_t + t0, d);
+            tc::wait_ld();
+            if (p.ranks > 1) {
 #pragma unroll
-            for (int t = 0; t < T; ++t)
-                if (t < tokens) f8::store_y(p.y, p.y_type, static_cast<size_t>(m0 + t) * p.ldy + n0 + row, acc[t]);
-        }
-    } else {
-        float* part = reinterpret_cast<float*>(smem);  // [T][128]
-        if (sums) {
+                for (int t = 0; t < 16; ++t) part[(t0 + t) * 128 + row] = __uint_as_float(d[t]);
+            } else if (n0 + row < p.N) {
 #pragma unroll
-            for (int t = 0; t < T; ++t) part[t * 128 + row] = acc[t];
+                for (int t = 0; t < 16; ++t)
+                    if (t0 + t < tokens) f8::store_y(p.y, p.y_type, static_cast<size_t>(m0 + t0 + t) * p.ldy + n0 + row, __uint_as_float(d[t]));
+            }
         }
+    }
+    if (p.ranks > 1) {
         cluster_sync_all();
-        if (sums && n0 + row < p.N) {
-            for (int t = rank; t < tokens; t += p.ranks) {
-                const uint32_t at = base + 4u * (t * 128 + row);
+        // every CTA adds a share of the tokens, 128 rows of one per four warps
+        const int turns = C::THREADS / 128, turn = tid >> 7, r128 = tid & 127;
+        if (turn < turns && n0 + r128 < p.N) {
+            for (int t = rank + p.ranks * turn; t < tokens; t += p.ranks * turns) {
+                const uint32_t at = base + 4u * (t * 128 + r128);
                 float v[kFewMaxCluster];
 #pragma unroll
                 for (int r = 0; r < kFewMaxCluster; ++r) {
@@ -279,11 +290,15 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                 float y = v[0];
 #pragma unroll
                 for (int r = 1; r < kFewMaxCluster; ++r) y += v[r];
-                f8::store_y(p.y, p.y_type, static_cast<size_t>(m0 + t) * p.ldy + n0 + row, y);
+                f8::store_y(p.y, p.y_type, static_cast<size_t>(m0 + t) * p.ldy + n0 + r128, y);
             }
         }
         cluster_sync_all();                            // the others may still read this CTA's sums
     }
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    if (warp == 1) tc::dealloc(tmem, C::TMEM);
     if (tid == 0 && *abort != 0) report_timeout(p.status, false);
 }
 
@@ -314,7 +329,7 @@ static cudaError_t few_launch(const Fp8Args& a) {
     }
     FewParams p;
     memset(&p, 0, sizeof p);
-    p.x = a.x; p.ldx = a.ldx; p.x_scales = reinterpret_cast<const uint8_t*>(a.x_scales); p.scales = a.scales; p.y = a.y; p.ldy = a.ldy;
+    p.x = a.x; p.ldx = a.ldx; p.x_scales = a.x_scales; p.scales = a.scales; p.y = a.y; p.ldy = a.ldy;
     p.status = reinterpret_cast<unsigned int*>(a.workspace);
     p.y_type = a.y_type; p.M = a.M; p.N = a.N; p.K = a.K; p.G = (a.K + f8::kBlock - 1) / f8::kBlock; p.Mp = a.Mp;
     CUtensorMap w_map, x_map;
@@ -322,11 +337,11 @@ static cudaError_t few_launch(const Fp8Args& a) {
     if (C::TAKES_X) x_map = w_map;                    // not used
     else if (!make_byte_map(&x_map, a.x_codes, a.M, a.K, T)) return cudaErrorUnknown;
     const long long tiles = static_cast<long long>((a.N + 127) / 128) * ((a.M + T - 1) / T);
-    p.ranks = few_cluster(tiles, p.G, C::PER_SM * device_sm_count());
+    p.ranks = few_cluster(tiles, p.G, 2 * device_sm_count());
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     cfg.gridDim = dim3(static_cast<unsigned>(tiles * p.ranks), 1, 1);
-    cfg.blockDim = dim3(kFewThreads, 1, 1);
+    cfg.blockDim = dim3(C::THREADS, 1, 1);
     cfg.dynamicSmemBytes = C::SMEM;
     cfg.stream = a.stream;
     cudaLaunchAttribute attr[2];

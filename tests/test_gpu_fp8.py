@@ -28,12 +28,12 @@ def _x(M, K, seed, kind="fp16"):
 
 
 def _check(y, x, codes, scales):
-    """Products of two e4m3 values are exact in fp32; a block's 128 are summed by the tensor cores (one truncation each at worst,
-    2^-23 of what the terms add up to in magnitude), the blocks in fp32 (2^-24 each, and twice for the scales' product), then one rounding to y."""
+    """Products of two e4m3 values, and their products with powers of two, are exact in fp32.  The tensor cores add 32 of them to the
+    accumulator at a time; over K columns that is K / 32 roundings of at most 2^-23 of what the terms add up to in magnitude (128 of them are allowed
+    beside, for what is lost when 33 terms are lined up), then one rounding to y."""
     want, mag = orc.linear(x.double().cpu().numpy(), codes.view(torch.uint8).cpu().numpy(), scales.double().cpu().numpy())
-    blocks = -(-codes.shape[1] // 128)
     half = torch.finfo(y.dtype).eps / 2
-    tol = (128 * 2.0 ** -23 + (blocks + 2) * 2.0 ** -24) * mag + half * np.abs(want) + (2.0 ** -25 if y.dtype == torch.float16 else 0.0)
+    tol = (128 + codes.shape[1] / 32) * 2.0 ** -23 * mag + half * np.abs(want) + (2.0 ** -25 if y.dtype == torch.float16 else 0.0)
     err = np.abs(y.double().cpu().numpy() - want)
     assert np.isfinite(err).all()
     assert (err <= tol).all(), (err / np.maximum(tol, 1e-300)).max()
@@ -86,17 +86,22 @@ def test_linear(M, N, K, kind, out):
 
 
 @pytest.mark.parametrize("M", [3, 40, 200])
-def test_any_scales(M):
-    """Scales that the quantizer would not give: not powers of two, of either sign, zero."""
+def test_scales_of_every_block_count(M):
+    """Scales that differ by many powers of two from block to block, and others than the quantizer would give: each block under its own."""
     slim = _slim()
-    N, K = 400, 700 // 16 * 16
-    layer = slim.Fp8Linear.from_weight(_weight(N, K, 5).cuda())
+    N, K = 400, 1296
+    codes, scales = slim.fp8_quantize(_weight(N, K, 5).cuda())
     g = torch.Generator().manual_seed(9)
-    scales = (torch.randn(layer.scales.shape, generator=g) * 0.01).cuda()
-    scales[1, 2] = 0.0
-    layer = slim.Fp8Linear(layer.codes, scales)
-    x = _x(M, K, 3).cuda()
-    _check(layer.forward(x, layer.new_workspace(M), out_dtype=torch.float32), x, layer.codes, scales)
+    scales = torch.exp2(torch.randint(-12, 4, scales.shape, generator=g).float()).cuda()
+    layer = slim.Fp8Linear(codes, scales)
+    x = _x(M, K, 3)
+    x *= torch.exp2(torch.arange(K) // 128 % 5 - 2.0).half()
+    x = (x.float() * torch.exp2(torch.randint(-3, 4, (M, 1), generator=g).float())).half().cuda()
+    _check(layer.forward(x, layer.new_workspace(M), out_dtype=torch.float32), x, codes, scales)
+    with pytest.raises(ValueError):
+        slim.Fp8Linear(codes, scales * 1.5)
+    with pytest.raises(ValueError):
+        slim.Fp8Linear(codes, -scales)
 
 
 @pytest.mark.parametrize("kind", ["fp16", "bf16"])
