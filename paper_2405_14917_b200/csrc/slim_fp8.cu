@@ -97,8 +97,8 @@ __global__ void __launch_bounds__(256) fp8_quantize_kernel(const T* __restrict__
 template <typename T>
 __global__ void __launch_bounds__(256) fp8_stage_kernel(const T* __restrict__ x, long long ld, uint8_t* __restrict__ codes,
                                                         uint32_t* __restrict__ scales, int M, int K, int words, int Mp) {
-    pdl_launch_dependents();
     pdl_wait();
+    pdl_launch_dependents();                           // in this order: the kernel behind may read W at once
     const long long unit = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) >> 4;
     const int c = threadIdx.x & 15;
     const int m = static_cast<int>(unit / words), j = static_cast<int>(unit - static_cast<long long>(m) * words);

@@ -104,6 +104,25 @@ __device__ __forceinline__ void store_y(void* y, int type, size_t at, float v) {
     else static_cast<__nv_bfloat16*>(y)[at] = __float2bfloat16_rn(v);
 }
 
+// n <= 16 of them, a row stride apart.
+__device__ __forceinline__ void store_column(void* y, int type, size_t at, long long ld, const uint32_t* d, int n) {
+    if (type == SLIM_F32) {
+        float* o = static_cast<float*>(y) + at;
+#pragma unroll
+        for (int t = 0; t < 16; ++t, o += ld)
+            if (t < n) *o = __uint_as_float(d[t]);
+    } else if (type == SLIM_F16) {
+        __half* o = static_cast<__half*>(y) + at;
+#pragma unroll
+        for (int t = 0; t < 16; ++t, o += ld)
+            if (t < n) *o = __float2half_rn(__uint_as_float(d[t]));
+    } else {
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(y) + at;
+#pragma unroll
+        for (int t = 0; t < 16; ++t, o += ld)
+            if (t < n) *o = __float2bfloat16_rn(__uint_as_float(d[t]));
+    }
+}
 // 32 lanes x 16 columns of 32 bits
 __device__ __forceinline__ void ld16(uint32_t taddr, uint32_t* v) {
     asm volatile(

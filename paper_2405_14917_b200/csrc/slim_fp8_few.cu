@@ -7,9 +7,9 @@
 // r / 32, the same in all lane quarters) into a buffer per slot.  At the end the CTAs of a cluster add their sums through
 // distributed shared memory, every CTA a share of the tokens, in rank order: no workspace, no second kernel, one result.
 //
-// Up to 32 tokens x is quantised here (TAKES_X), by four warps ahead of the MMAs, from x itself: every CTA does it for its part of K,
+// Up to 32 tokens x is quantised here (TAKES_X), by four warps that take the blocks in turn, from x itself: every CTA does it for its part of K,
 // which costs L2 reads of 2 T bytes per 128 bytes of W and saves the launch of the quantizer.  Beyond, the codes come
-// by TMA from the workspace (slim_fp8.cu).
+// by TMA from the workspace (slim_fp8.cu); W is then requested while the quantizer still runs.
 //
 // Warps: 0 loads of W (and of staged x); 1 MMAs, tensor memory; 4 to 7 scales, then the output (tensor-memory lanes 32 (w % 4) on); 2, 3, 8, 9
 // quantisation of x.  Every wait is bounded and reports through the workspace status word.
@@ -26,13 +26,16 @@ template <int T> struct FewCfg {
     static constexpr bool TAKES_X = T <= 32;
     static constexpr int THREADS = TAKES_X ? 320 : 256;
     static constexpr int W_BYTES = 128 * 128, X_BYTES = T * 128;
-    static constexpr int STAGES = T <= 32 ? 5 : T <= 64 ? 4 : 3;
-    static constexpr int AHEAD = T <= 16 ? 4 : 2;                         // blocks of x on their way to the quantising warps
+    static constexpr int STAGES = T <= 16 ? 5 : T <= 32 ? 4 : 3;
+    static constexpr int XSHARE = T / 16;                                 // warps that quantise a block together, 16 tokens each
+    static constexpr bool OWN_RECV = T <= 64;                             // the others' sums have a place of their own, not the ring's
     static constexpr int COL_SF = T;                                      // tensor memory: D, then per slot 4 columns of W's scales and T / 32 of x's
     static constexpr int TMEM_USED = T + 8 * STAGES;
     static constexpr int TMEM = TMEM_USED <= 64 ? 64 : TMEM_USED <= 128 ? 128 : 256;
     static constexpr int OFF_SX = STAGES * (W_BYTES + X_BYTES);           // TAKES_X: [STAGES][T] scale exponents
-    static constexpr int OFF_BAR = OFF_SX + STAGES * T;
+    static constexpr int OFF_RECV = OWN_RECV ? OFF_SX + STAGES * T : 0;   // [ranks][share of the tokens][128] fp32
+    static constexpr int RECV = (T + 8) * 512;
+    static constexpr int OFF_BAR = OFF_SX + STAGES * T + (OWN_RECV ? RECV : 0);
     static constexpr int SMEM = OFF_BAR + 256 + 1024;                     // + alignment of the slots
 };
 
@@ -85,12 +88,16 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
         *abort = 0;
         for (int s = 0; s < C::STAGES; ++s) {
             sb::init(w_full(s), 1);
-            sb::init(x_full(s), kFewXWarps);
+            sb::init(x_full(s), C::XSHARE);
             sb::init(sf_full(s), 4);
             sb::init(empty(s), 1);
         }
         sb::init(d_full, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&w_map)) : "memory");
+        if (!C::TAKES_X) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&x_map)) : "memory");
     }
     if (warp == 1) {
         tc::alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), C::TMEM);
@@ -106,7 +113,20 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
     __syncthreads();
     tc::fence_after();
     const uint32_t tmem = tc::uniform(*tmem_slot);
+    const bool meet = C::OWN_RECV && p.ranks > 1;
+    if (meet) cluster_arrive_relaxed();                // a CTA is written to only when it is known to have started
     pdl_launch_dependents();
+    // The kernel ahead of staged x is its quantizer, which lets this one start only when all before it has completed: W is there.
+    int first = 0;                                     // blocks of W requested ahead
+    if (!C::TAKES_X && warp == 0) {
+        first = min(steps, C::STAGES);
+        if (tc::elect())
+            for (int i = 0; i < first; ++i) {
+                sb::expect_tx(w_full(i), C::W_BYTES + C::X_BYTES);
+                tc::tma_load_2d(base + i * C::W_BYTES, &w_map, 128 * (g0 + i), n0, w_full(i));
+            }
+        __syncwarp();
+    }
     pdl_wait();
 
     if (warp == 0) {
@@ -116,8 +136,10 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
         for (int i = 0; i < steps; ++i) {
             if (!tc::warp_wait(empty(s), ph ^ 1u, abort)) break;
             if (tc::elect()) {
-                sb::expect_tx(w_full(s), C::TAKES_X ? C::W_BYTES : C::W_BYTES + C::X_BYTES);
-                tc::tma_load_2d(base + s * C::W_BYTES, &w_map, 128 * (g0 + i), n0, w_full(s));
+                if (i >= first) {
+                    sb::expect_tx(w_full(s), C::TAKES_X ? C::W_BYTES : C::W_BYTES + C::X_BYTES);
+                    tc::tma_load_2d(base + s * C::W_BYTES, &w_map, 128 * (g0 + i), n0, w_full(s));
+                }
                 if (!C::TAKES_X) tc::tma_load_2d(s_x + s * C::X_BYTES, &x_map, 128 * (g0 + i), m0, w_full(s));
             }
             __syncwarp();
@@ -189,48 +211,41 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             if (++s == C::STAGES) { s = 0; ph ^= 1u; }
         }
     } else if (C::TAKES_X) {
-        // ---- x into codes: half a warp per token and block, two tokens of a warp at a time
-        const int xw = warp < 4 ? warp - 2 : warp - 6;
-        constexpr int PAIRS = T / 2 / kFewXWarps;                         // pairs of tokens of a warp
+        // ---- x into codes: half a warp per token and block, two tokens of a warp at a time, a block in kFewXWarps / XSHARE per group of warps
+        const int xw = warp < 4 ? warp - 2 : warp - 6, part = xw % C::XSHARE;
+        constexpr int TURNS = kFewXWarps / C::XSHARE;
         const int half = lane >> 4, c = lane & 15;
-        const X* x = static_cast<const X*>(p.x);
-        uint4 v[C::AHEAD][PAIRS];
-        auto fetch = [&](int i, uint4* o) {
+        const X* x = static_cast<const X*>(p.x) + static_cast<size_t>(m0) * p.ldx;
+        uint4 v[8];
+        auto fetch = [&](int i) {
 #pragma unroll
-            for (int u = 0; u < PAIRS; ++u) {
-                const int t = 2 * (xw + kFewXWarps * u) + half, k = 128 * (g0 + i) + 8 * c;
-                o[u] = i < steps && t < tokens && k < p.K ? __ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(m0 + t) * p.ldx + k)) : make_uint4(0, 0, 0, 0);
+            for (int u = 0; u < 8; ++u) {
+                const int t = 16 * part + 2 * u + half, k = 128 * (g0 + i) + 8 * c;
+                v[u] = i < steps && t < tokens && k < p.K ? __ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(t) * p.ldx + k)) : make_uint4(0, 0, 0, 0);
             }
         };
-#pragma unroll
-        for (int a = 0; a < C::AHEAD; ++a) fetch(a, v[a]);
-        int s = 0;
+        int s = xw / C::XSHARE;                        // below the number of slots
         uint32_t ph = 0;
-        bool ok = true;
-        for (int i0 = 0; i0 < steps && ok; i0 += C::AHEAD) {
+        fetch(s);
+        for (int i = s; i < steps; i += TURNS) {
+            if (!tc::warp_wait(empty(s), ph ^ 1u, abort)) break;
 #pragma unroll
-            for (int a = 0; a < C::AHEAD; ++a) {
-                const int i = i0 + a;
-                if (i >= steps) break;
-                ok = tc::warp_wait(empty(s), ph ^ 1u, abort);
-                if (!ok) break;
-#pragma unroll
-                for (int u = 0; u < PAIRS; ++u) {
-                    const int t = 2 * (xw + kFewXWarps * u) + half;
-                    if (2 * (xw + kFewXWarps * u) >= tokens) continue;
-                    uint32_t e;
-                    const uint2 codes = f8::quantise8<X>(v[a][u], e);
-                    // row t of a swizzled tile: its 16-byte chunks stand at chunk ^ (t & 7)
-                    const uint32_t at = s_x + s * C::X_BYTES + t * 128 + ((((c >> 1) ^ (t & 7)) << 4) | ((c & 1) << 3));
-                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(codes.x), "r"(codes.y) : "memory");
-                    if (c == 0) smem[C::OFF_SX + s * T + t] = static_cast<uint8_t>(e);
-                }
-                fetch(i + C::AHEAD, v[a]);
-                tc::fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) sb::arrive(x_full(s));
-                if (++s == C::STAGES) { s = 0; ph ^= 1u; }
+            for (int u = 0; u < 8; ++u) {
+                const int t = 16 * part + 2 * u + half;
+                if (16 * part + 2 * u >= tokens) break;
+                uint32_t e;
+                const uint2 codes = f8::quantise8<X>(v[u], e);
+                // row t of a swizzled tile: its 16-byte chunks stand at chunk ^ (t & 7)
+                const uint32_t at = s_x + s * C::X_BYTES + t * 128 + ((((c >> 1) ^ (t & 7)) << 4) | ((c & 1) << 3));
+                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(codes.x), "r"(codes.y) : "memory");
+                if (c == 0) smem[C::OFF_SX + s * T + t] = static_cast<uint8_t>(e);
             }
+            fetch(i + TURNS);
+            tc::fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) sb::arrive(x_full(s));
+            s += TURNS;
+            if (s >= C::STAGES) { s -= C::STAGES; ph ^= 1u; }
         }
     }
 
@@ -247,14 +262,15 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             if (tc::elect()) { f8::drain(empty(s), 0); f8::drain(empty(s), 1); }
             __syncwarp();
         }
-    (void)done;
-    __syncthreads();
+    if (meet) cluster_wait();
+    if (!C::OWN_RECV && p.ranks > 1) cluster_sync_all();      // everyone's ring is free
+    else __syncthreads();
     tc::fence_after();
-    const int row = 32 * (warp & 3) + lane;            // warps 4 to 7
-    const bool sums = warp >= 4 && warp < 8;
-    const uint32_t d_t = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
-    float* part = reinterpret_cast<float*>(smem);      // [T][128], in the ring
-    if (sums) {
+    if (warp >= 4 && warp < 8 && done) {
+        const int row = 32 * (warp & 3) + lane;
+        const uint32_t d_t = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
+        int owner = 0, u = 0;                          // of the token: its CTA, its place there
+        const int share = (tokens + p.ranks - 1) / p.ranks;
 #pragma unroll 1
         for (int t0 = 0; t0 < tokens; t0 += 16) {
             uint32_t d[16];
@@ -262,38 +278,36 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             tc::wait_ld();
             if (p.ranks > 1) {
 #pragma unroll
-                for (int t = 0; t < 16; ++t) part[(t0 + t) * 128 + row] = __uint_as_float(d[t]);
+                for (int t = 0; t < 16; ++t) {
+                    if (t0 + t < tokens) {
+                        uint32_t remote;
+                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(base + C::OFF_RECV + 4u * ((rank * share + u) * 128 + row)), "r"(owner));
+                        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(remote), "r"(d[t]) : "memory");
+                    }
+                    if (++owner == p.ranks) { owner = 0; ++u; }
+                }
             } else if (n0 + row < p.N) {
-#pragma unroll
-                for (int t = 0; t < 16; ++t)
-                    if (t0 + t < tokens) f8::store_y(p.y, p.y_type, static_cast<size_t>(m0 + t0 + t) * p.ldy + n0 + row, __uint_as_float(d[t]));
+                const size_t at = static_cast<size_t>(m0 + t0) * p.ldy + n0 + row;
+                const int n = min(16, tokens - t0);
+                f8::store_column(p.y, p.y_type, at, p.ldy, d, n);
             }
         }
     }
     if (p.ranks > 1) {
         cluster_sync_all();
-        // every CTA adds a share of the tokens, 128 rows of one per four warps
-        const int turns = C::THREADS / 128, turn = tid >> 7, r128 = tid & 127;
-        if (turn < turns && n0 + r128 < p.N) {
-            for (int t = rank + p.ranks * turn; t < tokens; t += p.ranks * turns) {
-                const uint32_t at = base + 4u * (t * 128 + r128);
-                float v[kFewMaxCluster];
+        // every CTA adds its share of the tokens, 128 rows of one per four warps
+        constexpr int turns = C::THREADS / 128;
+        const int turn = tid >> 7, row = tid & 127, share = (tokens + p.ranks - 1) / p.ranks;
+        if (turn < turns && n0 + row < p.N) {
+            const float* recv = reinterpret_cast<const float*>(smem + C::OFF_RECV) + row;
+            for (int u = turn; rank + p.ranks * u < tokens; u += turns) {
+                float y = recv[u * 128];
 #pragma unroll
-                for (int r = 0; r < kFewMaxCluster; ++r) {
-                    uint32_t remote;
-                    v[r] = 0.f;
-                    if (r < p.ranks) {
-                        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(r));
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(remote) : "memory");
-                    }
-                }
-                float y = v[0];
-#pragma unroll
-                for (int r = 1; r < kFewMaxCluster; ++r) y += v[r];
-                f8::store_y(p.y, p.y_type, static_cast<size_t>(m0 + t) * p.ldy + n0 + r128, y);
+                for (int r = 1; r < kFewMaxCluster; ++r)
+                    if (r < p.ranks) y += recv[(r * share + u) * 128];
+                f8::store_y(p.y, p.y_type, static_cast<size_t>(m0 + rank + p.ranks * u) * p.ldy + n0 + row, y);
             }
         }
-        cluster_sync_all();                            // the others may still read this CTA's sums
     }
     tc::fence_before();
     __syncthreads();

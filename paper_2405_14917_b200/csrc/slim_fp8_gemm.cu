@@ -117,13 +117,24 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
     tc::fence_after();
     const uint32_t tmem = tc::uniform(*tmem_slot);
     pdl_launch_dependents();
+    // The kernel ahead is the quantizer of x, which lets this one start only when all before it has completed: W is there, and requested at once.
+    const uint32_t bytes = (128u + static_cast<uint32_t>(feat) / 2u) * 128u;
+    int first = 0;                                     // blocks of W requested ahead
+    if (warp == 0) {
+        first = min(G, kFgStages);
+        if (tc::elect())
+            for (int i = 0; i < first; ++i) {
+                sb::expect_tx(full(i), bytes);
+                tc::tma_load_2d(base + i * kFgSlot + kFgSlot / 2, &w_map, 128 * i, pair / p.tok_tiles * feat + feat / 2 * rank, full(i));
+            }
+        __syncwarp();
+    }
     pdl_wait();
 
     int issued = 0;                                    // blocks this role has begun
     if (warp < 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFgRegsFew));
         if (warp == 0) {
-            const uint32_t bytes = (128u + static_cast<uint32_t>(feat) / 2u) * 128u;
             for (int tile = pair; tile < p.tiles; tile += pairs) {
                 const int m0 = tile % p.tok_tiles * kFgTok + 128 * rank, n0 = tile / p.tok_tiles * feat + feat / 2 * rank;
                 int g = 0;
@@ -131,9 +142,11 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                     const int s = issued % kFgStages;
                     if (!tc::warp_wait(empty(s), ((issued / kFgStages) & 1u) ^ 1u, abort)) break;
                     if (tc::elect()) {
-                        sb::expect_tx(full(s), bytes);
+                        if (issued >= first) {
+                            sb::expect_tx(full(s), bytes);
+                            tc::tma_load_2d(base + s * kFgSlot + kFgSlot / 2, &w_map, 128 * g, n0, full(s));
+                        }
                         tc::tma_load_2d(base + s * kFgSlot, &x_map, 128 * g, m0, full(s));
-                        tc::tma_load_2d(base + s * kFgSlot + kFgSlot / 2, &w_map, 128 * g, n0, full(s));
                     }
                     __syncwarp();
                 }
