@@ -109,15 +109,15 @@ __global__ void __launch_bounds__(256) fp8_stage_kernel(const T* __restrict__ x,
         const int k = (4 * j + i) * f8::kBlock + 8 * c;
         v[i] = m < M && k < K ? __ldg(reinterpret_cast<const uint4*>(row + k)) : make_uint4(0, 0, 0, 0);
     }
-    uint32_t word = 0;
+    uint2 q[4];
+    uint32_t e[4];
+    f8::quantise8<T>(v, q, e);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int k = (4 * j + i) * f8::kBlock + 8 * c;
-        uint32_t e;
-        const uint2 q = f8::quantise8<T>(v[i], e);
-        if (m < M && k < K) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(m) * K + k) = q;
-        word |= e << (8 * i);
+        if (m < M && k < K) *reinterpret_cast<uint2*>(codes + static_cast<size_t>(m) * K + k) = q[i];
     }
+    const uint32_t word = e[0] | e[1] << 8 | e[2] << 16 | e[3] << 24;
     if (c == 0 && m < M) scales[static_cast<size_t>(j) * Mp + m] = word;
 }
 

@@ -72,29 +72,48 @@ template <> struct Half16<__nv_bfloat16> {
 __device__ __forceinline__ uint32_t top2(const uint4& v) {
     return __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
 }
-// The block of 128 that half a warp holds, eight elements a lane: this lane's codes, and the scale's exponent.  All lanes of the warp take part.
-template <typename T>
-__device__ __forceinline__ uint2 quantise8(const uint4& v, uint32_t& exponent) {
-    uint32_t m = top2(v);
+// Blocks of 128 that half a warp holds, eight elements a lane and block: this lane's codes, and the scales' exponents.  All lanes of the warp take
+// part.  What is not finite is looked for once for all U blocks, so that their chains run side by side.
+template <typename T, int U>
+__device__ __forceinline__ void quantise8(const uint4 (&v)[U], uint2 (&codes)[U], uint32_t (&exponent)[U]) {
+    uint32_t m[U], most = 0;
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, o));
-    m = max(m & 0xffffu, m >> 16);
-    float f[8];
-    Half16<T>::unpack(v, f);
-    const bool finite = m < Half16<T>::INF;
-    uint32_t bits = __float_as_uint(Half16<T>::one(m));
-    if (__any_sync(0xffffffffu, !finite)) {
-        uint32_t mx = 0;
+    for (int u = 0; u < U; ++u) m[u] = top2(v[u]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mx = max(mx, magnitude(f[e]));
+    for (int o = 8; o > 0; o >>= 1)
 #pragma unroll
-        for (int o = 8; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        bits = mx;
+        for (int u = 0; u < U; ++u) m[u] = __vmaxu2(m[u], __shfl_xor_sync(0xffffffffu, m[u], o));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        m[u] = max(m[u] & 0xffffu, m[u] >> 16);
+        most = max(most, m[u]);
     }
-    const uint32_t sb = scale_bits(bits);
-    const float inv = inverse_scale(sb);
-    exponent = sb >> 23;
-    return finite ? make_uint2(codes4<false>(f, inv), codes4<false>(f + 4, inv)) : make_uint2(codes4<true>(f, inv), codes4<true>(f + 4, inv));
+    if (__any_sync(0xffffffffu, most >= Half16<T>::INF)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float f[8];
+            Half16<T>::unpack(v[u], f);
+            uint32_t mx = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mx = max(mx, magnitude(f[e]));
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const uint32_t sb = scale_bits(mx);
+            const float inv = inverse_scale(sb);
+            exponent[u] = sb >> 23;
+            codes[u] = make_uint2(codes4<true>(f, inv), codes4<true>(f + 4, inv));
+        }
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float f[8];
+        Half16<T>::unpack(v[u], f);
+        const uint32_t sb = scale_bits(__float_as_uint(Half16<T>::one(m[u])));
+        const float inv = inverse_scale(sb);
+        exponent[u] = sb >> 23;
+        codes[u] = make_uint2(codes4<false>(f, inv), codes4<false>(f + 4, inv));
+    }
 }
 
 // y element: `type` is SLIM_F32, SLIM_F16 or SLIM_BF16; one rounding of the fp32 sum.

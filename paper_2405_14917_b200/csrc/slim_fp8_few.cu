@@ -214,6 +214,7 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
         // ---- x into codes: half a warp per token and block, two tokens of a warp at a time, a block in kFewXWarps / XSHARE per group of warps
         const int xw = warp < 4 ? warp - 2 : warp - 6, part = xw % C::XSHARE;
         constexpr int TURNS = kFewXWarps / C::XSHARE;
+        static_assert(TURNS <= C::STAGES, "the first blocks of the warps have slots of their own");
         const int half = lane >> 4, c = lane & 15;
         const X* x = static_cast<const X*>(p.x) + static_cast<size_t>(m0) * p.ldx;
         uint4 v[8];
@@ -229,16 +230,28 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
         fetch(s);
         for (int i = s; i < steps; i += TURNS) {
             if (!tc::warp_wait(empty(s), ph ^ 1u, abort)) break;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int t = 16 * part + 2 * u + half;
-                if (16 * part + 2 * u >= tokens) break;
-                uint32_t e;
-                const uint2 codes = f8::quantise8<X>(v[u], e);
+            // tokens past the last are zeros, with codes of zeros
+            uint2 codes[8];
+            uint32_t e[8];
+            auto put = [&](int u) {
                 // row t of a swizzled tile: its 16-byte chunks stand at chunk ^ (t & 7)
+                const int t = 16 * part + 2 * u + half;
                 const uint32_t at = s_x + s * C::X_BYTES + t * 128 + ((((c >> 1) ^ (t & 7)) << 4) | ((c & 1) << 3));
-                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(codes.x), "r"(codes.y) : "memory");
-                if (c == 0) smem[C::OFF_SX + s * T + t] = static_cast<uint8_t>(e);
+                asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(codes[u].x), "r"(codes[u].y) : "memory");
+                if (c == 0) smem[C::OFF_SX + s * T + t] = static_cast<uint8_t>(e[u]);
+            };
+            if (tokens <= 2) {                         // one pair: the others' slots are zero from the start
+                uint4 one[1] = {v[0]};
+                uint2 q[1];
+                uint32_t x1[1];
+                f8::quantise8<X>(one, q, x1);
+                codes[0] = q[0];
+                e[0] = x1[0];
+                put(0);
+            } else {
+                f8::quantise8<X>(v, codes, e);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) put(u);
             }
             fetch(i + TURNS);
             tc::fence_proxy_async();
