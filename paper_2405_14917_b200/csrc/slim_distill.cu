@@ -14,7 +14,7 @@
 // between the statistics and the gradient, so that the logits are not read again.  The slice statistics
 // meet through distributed shared memory; every sum has a fixed order.  Sums over the vocabulary are fp32 per thread (64 terms at a time) and fp64 from
 // there on; what is computed per row and per entry is fp64, because a small loss is the difference of large terms.
-#include "slim_gemv_dev.cuh"
+#include "slim_gemv_i8.cuh"
 
 #include <cuda_bf16.h>
 
@@ -463,6 +463,403 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     }
 }
 
+// ------------------------------------------------------------------------------------------ the one pass over many rows
+// With more rows than CTAs at once, a CTA (or cluster) takes row after row, and what a row waits for is done for the next one meanwhile, by a seventeenth
+// warp: it has the row brought into shared memory (one bulk copy), reads the entries and the logits at them, works out the teacher's
+// probabilities and marks the listed columns; when the sixteen have the row's statistics it computes its loss beside their
+// gradient.  They take the row from shared memory into registers at once, which frees the buffer for the next.  4096 x 32000 bf16 took 173 us with
+// a CTA per row (of 22000 cycles 9000 went until the entries were there and 4000 into the row's own terms), two per SM.
+// Statistics meet in a cluster by asynchronous stores that count on the receiver's barrier.  Every wait is bounded; rows left
+// undone by one that gives up have NaN for a loss.
+constexpr int kDsRowsThreads = kDsThreads + 32;
+
+struct RowTerms {            // what a row comes to, for its loss
+    float ref;
+    double R, Z, p_in, q_rest, p_rest;
+};
+
+template <typename T>
+struct RowsSmem {            // byte offsets
+    int row, entries, entry_stride, mark, total;
+    __host__ __device__ RowsSmem(int slice, int k, int mark_bytes) {
+        row = 0;
+        entries = (slice / DsType<T>::E + 1) * 16;
+        mark = entry_bytes(k);
+        entry_stride = mark + (mark_bytes + 15) / 16 * 16;
+        total = entries + 2 * entry_stride;
+    }
+};
+
+__device__ __forceinline__ void st_async_f32x2(uint32_t cluster_addr, float2 v, uint32_t cluster_bar) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                 ::"r"(cluster_addr), "f"(v.x), "f"(v.y), "r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ uint32_t map_cluster(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float redux_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+template <typename T, bool REST>
+__global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const DistillParams p) {
+    constexpr int E = DsType<T>::E;
+    extern __shared__ __align__(16) unsigned char ds_smem[];
+    const RowsSmem<T> lay(p.slice, p.k, p.mark_bytes);
+    __shared__ __align__(8) uint64_t s_bar[10];
+    __shared__ float2 s_part[2][kDsWarps];
+    __shared__ float2 s_slice[2][kDsMaxCluster];
+    __shared__ double s_teacher[2][2];                                 // the teacher's listed mass; whether there is any
+    __shared__ int s_twice[2];
+    __shared__ RowTerms s_terms[2];
+    __shared__ int s_abort;
+    volatile int* abort = &s_abort;
+    const uint32_t bar0 = smem_u32(s_bar);
+    const uint32_t row_full = bar0, row_empty = bar0 + 8;
+    auto ent_full = [&](int b) { return bar0 + 16u + 8u * b; };
+    auto ent_empty = [&](int b) { return bar0 + 32u + 8u * b; };
+    auto terms_full = [&](int b) { return bar0 + 48u + 8u * b; };
+    auto slice_full = [&](int b) { return bar0 + 64u + 8u * b; };
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int ranks = p.ranks, rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+    const int first = static_cast<int>(blockIdx.x) / ranks, stride = static_cast<int>(gridDim.x) / ranks;
+    const int v0 = min(p.V, rank * p.slice), v1 = min(p.V, v0 + p.slice);
+    if (tid == 0) {
+        s_abort = 0;
+        sb::init(row_full, 1);
+        sb::init(row_empty, kDsWarps);
+        for (int b = 0; b < 2; ++b) {
+            sb::init(ent_full(b), 1);
+            sb::init(ent_empty(b), kDsWarps);
+            sb::init(terms_full(b), 1);
+            sb::init(slice_full(b), 1);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    if (ranks > 1) cluster_sync_all();                 // the others' barriers exist
+    const T* logits = static_cast<const T*>(p.logits);
+    auto slice_of = [&](int row) { return Slice<T>(logits + static_cast<long long>(row) * p.ld + v0, v1 - v0); };
+    const double ln2 = 0.69314718055994530942, cd = p.c;
+
+    if (warp == kDsWarps) {
+        // ------------------------------------------------------------------ the seventeenth warp
+        auto entries = [&](int row, int n) {           // of the n-th row of this CTA; its buffers are free
+            const int b = n & 1;
+            unsigned char* e0 = ds_smem + lay.entries + b * lay.entry_stride;
+            double* s_q = reinterpret_cast<double*>(e0);
+            double* s_lq = s_q + p.k;
+            int* s_idx = reinterpret_cast<int*>(s_lq + p.k);
+            float* s_s = reinterpret_cast<float*>(s_idx + p.k + 4);
+            uint8_t* s_first = reinterpret_cast<uint8_t*>(s_s + p.k);
+            uint32_t* s_mark = reinterpret_cast<uint32_t*>(e0 + lay.mark);
+            const T* r_logits = logits + static_cast<long long>(row) * p.ld;
+            const Slice<T> sl = slice_of(row);
+            // what of the slice is not whole vectors
+            if (lane < 2 * E) {
+                const int j = lane < E ? 0 : sl.nv - 1, i = j * E + lane % E;
+                if (sl.nv > 0 && !sl.whole(j))
+                    reinterpret_cast<T*>(ds_smem + lay.row)[i] = i >= sl.shift && i < sl.end ? sl.base[i] : DsType<T>::round(-INFINITY);
+            }
+            double top = -INFINITY;
+            int any = 0, finite = 0, twice = 0;
+            for (int j = lane; j < p.k; j += 32) {
+                const size_t at = static_cast<size_t>(row) * p.k + j;
+                const long long i = p.index64 ? static_cast<const long long*>(p.index)[at] : static_cast<const int*>(p.index)[at];
+                const bool in = i >= 0 && i < p.V;
+                double u;
+                if (p.value_type == SLIM_F32) u = static_cast<const float*>(p.value)[at];
+                else if (p.value_type == SLIM_F16) u = __half2float(static_cast<const __half*>(p.value)[at]);
+                else u = __bfloat162float(static_cast<const __nv_bfloat16*>(p.value)[at]);
+                u *= p.inv_t;
+                s_idx[j] = in ? static_cast<int>(i) : -1;
+                s_s[j] = in ? DsType<T>::one(r_logits[i]) : 0.f;
+                s_lq[j] = u;
+                if (in) { top = fmax(top, u); any = 1; finite |= !(u == -INFINITY); }
+            }
+            if (lane < 4) s_idx[p.k + lane] = -1;
+            if (REST)
+                for (int j = lane; j < p.mark_bytes / 4; j += 32) s_mark[j] = 0u;
+            __syncwarp();
+            for (int j = lane; j < p.k; j += 32) {
+                const int i = s_idx[j];
+                bool again = false;
+                for (int o = 0; o < j; o += 4) {
+                    const int4 c = *reinterpret_cast<const int4*>(s_idx + o);
+                    again = again || (c.x == i) || (o + 1 < j && c.y == i) || (o + 2 < j && c.z == i) || (o + 3 < j && c.w == i);
+                }
+                s_first[j] = i >= 0 && !again;
+                twice |= i >= 0 && again;
+                if (REST && i >= v0 && i < v1) {
+                    const int e = i - v0 + sl.shift;
+                    atomicOr(s_mark + (e / E >> 2), 1u << ((e / E & 3) * 8 + e % E));
+                }
+            }
+            any = __any_sync(0xffffffffu, any);
+            double norm;
+            if (REST) norm = p.lse[row];
+            else {
+                any = __any_sync(0xffffffffu, finite);
+                top = warp_max(top);
+                double sum = 0.0;
+                for (int j = lane; j < p.k; j += 32)
+                    if (s_idx[j] >= 0) sum += exp(s_lq[j] - top);
+                norm = top + log(warp_sum(sum));
+            }
+            double q_sum = 0.0;
+            for (int j = lane; j < p.k; j += 32) {
+                const double lq = s_lq[j] - norm;
+                const double q = s_idx[j] >= 0 && any ? exp(lq) : 0.0;
+                s_lq[j] = lq;
+                s_q[j] = q;
+                q_sum += q;
+            }
+            q_sum = warp_sum(q_sum);
+            twice = __any_sync(0xffffffffu, twice);
+            if (lane == 0) { s_teacher[b][0] = q_sum; s_teacher[b][1] = any; s_twice[b] = twice; }
+            __syncwarp();
+            if (lane == 0) sb::arrive(ent_full(b));
+        };
+        auto bring = [&](int row) {                    // the whole vectors of the slice
+            const Slice<T> sl = slice_of(row);
+            const int from = sl.shift > 0 ? 1 : 0, to = sl.end / E;
+            const uint32_t bytes = to > from ? 16u * static_cast<uint32_t>(to - from) : 0u;
+            if (lane == 0) {
+                sb::expect_tx(row_full, bytes);
+                if (bytes > 0) sb::bulk_g2s(smem_u32(ds_smem) + lay.row + 16u * from, reinterpret_cast<const uint4*>(sl.base) + from, bytes, row_full);
+            }
+            __syncwarp();
+        };
+        int n = 0;
+        if (first < p.M) { bring(first); entries(first, 0); }
+        for (int row = first; row < p.M; row += stride, ++n) {
+            const int b = n & 1, next = row + stride;
+            bool ok = true;
+            if (next < p.M) {
+                ok = __all_sync(0xffffffffu, sb::wait(row_empty, n & 1u, abort));
+                if (ok) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the buffer was read, and its ends written, by ordinary accesses
+                    bring(next);
+                    if (n > 0) ok = __all_sync(0xffffffffu, sb::wait(ent_empty(b ^ 1), ((n - 1) >> 1) & 1u, abort));
+                }
+                if (ok) entries(next, n + 1);
+            }
+            ok = ok && __all_sync(0xffffffffu, sb::wait(terms_full(b), (n >> 1) & 1u, abort));
+            if (!ok) {
+                for (int r = row; r < p.M && rank == 0; r += stride)
+                    if (lane == 0) p.loss[r] = NAN;
+                break;
+            }
+            if (rank != 0) continue;
+            const RowTerms t = s_terms[b];
+            unsigned char* e0 = ds_smem + lay.entries + b * lay.entry_stride;
+            const double* s_q = reinterpret_cast<const double*>(e0);
+            const double* s_lq = s_q + p.k;
+            const int* s_idx = reinterpret_cast<const int*>(s_lq + p.k);
+            const float* s_s = reinterpret_cast<const float*>(s_idx + p.k + 4);
+            const double lz = log(t.Z);
+            double l = 0.0;
+            for (int j = lane; j < p.k; j += 32) {
+                const double q = s_q[j];
+                if (s_idx[j] < 0 || q == 0.0) continue;
+                l += q * (s_lq[j] - (t.Z == 0.0 ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lz));
+            }
+            l = warp_sum(l);
+            if (REST && !(t.q_rest == 0.0))
+                l += t.q_rest * (log(t.q_rest) - (t.p_rest == 0.0 ? -INFINITY : t.p_in < 0.5 ? log1p(-t.p_in) : log(t.p_rest)));
+            if (lane == 0) p.loss[row] = s_teacher[b][1] != 0.0 ? static_cast<float>(l) : 0.f;
+        }
+    } else {
+        // ------------------------------------------------------------------ the sixteen
+        const uint64_t c2 = pair2(p.c, p.c);
+        auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(kDsThreads) : "memory"); };
+        int n = 0;
+        for (int row = first; row < p.M; row += stride, ++n) {
+            const int b = n & 1;
+            const uint32_t ph = (n >> 1) & 1u;
+            const unsigned char* e0 = ds_smem + lay.entries + b * lay.entry_stride;
+            const double* s_q = reinterpret_cast<const double*>(e0);
+            const int* s_idx = reinterpret_cast<const int*>(s_q + 2 * p.k);
+            const float* s_s = reinterpret_cast<const float*>(s_idx + p.k + 4);
+            const uint8_t* s_first = reinterpret_cast<const uint8_t*>(s_s + p.k);
+            const uint8_t* mark = e0 + lay.mark;
+            const Slice<T> sl = slice_of(row);
+            const float weight = p.dloss[row];
+            // a warp that gives up says so to the others at the next meeting; all leave there
+            bool ok = sb::wait(ent_full(b), ph, abort);
+            ok = sb::wait(row_full, n & 1u, abort) && ok;
+            __syncwarp();
+            const uint4* buf = reinterpret_cast<const uint4*>(ds_smem + lay.row) + tid;
+            const float ninf = -INFINITY;
+            uint4 x[kDsVecs];
+#pragma unroll
+            for (int u = 0; u < kDsVecs; ++u) {
+                if (tid + u * kDsThreads < sl.nv) x[u] = buf[u * kDsThreads];
+                else {
+                    float f[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) f[e] = ninf;
+                    x[u] = DsType<T>::pack(f);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) sb::arrive(row_empty);
+
+            // ---- maximum and sum of exponentials (outside the set with REST) of a warp, the slice, the row
+            const float tm = redux_max(vec_max(x, kDsVecs, static_cast<const T*>(nullptr)));
+            float ws;
+            {
+                const float neg = tm == -INFINITY ? 0.f : -tm;
+                const uint64_t neg2 = pair2(neg, neg);
+                uint64_t acc = pair2(0.f, 0.f);
+#pragma unroll
+                for (int u = 0; u < kDsVecs; ++u) {
+                    forget(x[u]);
+                    const int j = tid + u * kDsThreads;
+                    if (j < sl.nv) {
+                        float f[E];
+                        DsType<T>::unpack(x[u], f);
+                        if (REST) {
+                            const uint32_t m = mark[j];
+                            if (m != 0) {
+#pragma unroll
+                                for (int e = 0; e < E; ++e)
+                                    if (m >> e & 1u) f[e] = -INFINITY;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < E; e += 2) {
+                            float v, w;
+                            unpair2(mul2(add2(pair2(f[e], f[e + 1]), neg2), c2), v, w);
+                            acc = add2(acc, pair2(ex2(v), ex2(w)));
+                        }
+                    }
+                }
+                float v, w;
+                unpair2(acc, v, w);
+                ws = v + w;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
+            if (lane == 0) s_part[b][warp] = make_float2(tm, ws);
+            meet();
+            float m;
+            double R;
+            auto join = [&](float2 part, bool in) {
+                m = redux_max(in ? part.x : -INFINITY);
+                double v = !in ? 0.0 : part.x == -INFINITY ? static_cast<double>(part.y) : static_cast<double>(part.y * ex2((part.x - m) * p.c));
+#pragma unroll
+                for (int o = kDsWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);       // in the low and the high half of the warp alike
+                R = __shfl_sync(0xffffffffu, v, 0);
+            };
+            join(s_part[b][lane % kDsWarps], lane < kDsWarps);
+            if (ranks > 1) {
+                if (tid == 0) sb::expect_tx(slice_full(b), 8u * ranks);
+                if (tid < ranks)
+                    st_async_f32x2(map_cluster(smem_u32(&s_slice[b][rank]), tid), make_float2(m, static_cast<float>(R)), map_cluster(slice_full(b), tid));
+                ok = sb::wait(slice_full(b), ph, abort) && ok;
+                __syncwarp();
+                join(s_slice[b][lane % ranks], lane < ranks);
+            }
+
+            // ---- what the row comes to, by every warp for itself
+            const float ref = m == -INFINITY ? 0.f : m;
+            const double q_sum = s_teacher[b][0];
+            const bool any = s_teacher[b][1] != 0.0;
+            double Z = R, p_rest = 0.0, q_rest = 0.0;
+            float p_in = 0.f;
+            bool little = false;                       // the set has less than half of the mass: the rest is what it leaves of 1
+            if (REST) {
+                float z = 0.f;
+                int columns = 0;
+                for (int j = lane; j < p.k; j += 32)
+                    if (s_first[j]) { z += ex2((s_s[j] - ref) * p.c); ++columns; }
+                const double zd = warp_sum(static_cast<double>(z));
+                Z += zd;
+                p_in = Z == 0.0 ? 0.f : static_cast<float>(zd) / static_cast<float>(Z);
+                little = p_in < 0.5f;
+                p_rest = Z == 0.0 ? 0.0 : little ? 1.0 - static_cast<double>(p_in) : static_cast<double>(static_cast<float>(R) / static_cast<float>(Z));
+                q_rest = static_cast<int>(__reduce_add_sync(0xffffffffu, columns)) < p.V ? fmax(1.0 - q_sum, 0.0) : 0.0;
+                if (q_sum != q_sum) q_rest = q_sum;    // a NaN among the teacher's values
+            }
+            if (tid == 0) {
+                RowTerms t;
+                t.ref = ref; t.R = R; t.Z = Z; t.p_in = p_in; t.q_rest = q_rest; t.p_rest = p_rest;
+                s_terms[b] = t;
+                sb::arrive(terms_full(b));
+            }
+            const double d = static_cast<double>(weight) * p.inv_t;
+            const float inv_z = Z == 0.0 ? 0.f : 1.f / static_cast<float>(Z);
+            const double mass = q_sum + q_rest;
+            float other = static_cast<float>(mass);
+            if (REST && !(q_rest == 0.0))
+                other = p_rest == 0.0 ? 0.f : static_cast<float>(little ? q_sum - static_cast<double>(p_in) : p_rest - q_rest) / static_cast<float>(p_rest);
+            const float factor = any ? other * inv_z * static_cast<float>(d) : 0.f;
+
+            // ---- the gradient: one factor for the whole row, then the listed columns
+            T* r_grad = static_cast<T*>(p.grad) + static_cast<long long>(row) * p.ldg;
+            T* g_base = r_grad + v0 - sl.shift;
+            const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
+            const uint64_t neg2 = pair2(-ref, -ref), factor2 = pair2(factor, factor);
+#pragma unroll
+            for (int u = 0; u < kDsVecs; ++u) {
+                forget(x[u]);
+                const int j = tid + u * kDsThreads;
+                if (j < sl.nv) {
+                    float f[E];
+                    DsType<T>::unpack(x[u], f);
+#pragma unroll
+                    for (int e = 0; e < E; e += 2) {
+                        float v, w;
+                        unpair2(mul2(add2(pair2(f[e], f[e + 1]), neg2), c2), v, w);
+                        unpair2(mul2(pair2(ex2(v), ex2(w)), factor2), f[e], f[e + 1]);
+                    }
+                    if (!any) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) f[e] = 0.f;
+                    }
+                    if (vectors && sl.whole(j)) __stcs(reinterpret_cast<uint4*>(g_base) + j, DsType<T>::pack(f));
+                    else {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const int i = j * E + e;
+                            if (i >= sl.shift && i < sl.end) g_base[i] = DsType<T>::round(f[e]);
+                        }
+                    }
+                }
+            }
+            uint32_t gave_up;                          // the listed columns are written over; and who has given up says so
+            asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                         : "=r"(gave_up) : "r"(ok ? 0u : 1u), "n"(kDsThreads) : "memory");
+            if (any) {
+                for (int j = tid; j < p.k; j += kDsThreads) {
+                    const int i = s_idx[j];
+                    if (!s_first[j] || i < v0 || i >= v1) continue;
+                    double q = s_q[j];
+                    if (s_twice[b])
+                        for (int o = j + 1; o < p.k; ++o) q += s_idx[o] == i ? s_q[o] : 0.0;
+                    r_grad[i] = DsType<T>::round(static_cast<float>((static_cast<double>(ex2((s_s[j] - ref) * p.c) * inv_z) * mass - q) * d));
+                }
+            }
+            __syncwarp();
+            if (lane == 0) sb::arrive(ent_empty(b));
+            if (gave_up) break;
+        }
+    }
+    // after a wait that gave up a copy may still be on its way to this CTA's shared memory, or the others' statistics
+    if (*abort != 0 && tid == kDsThreads) {
+        const unsigned long long t0 = sb::timer_ns();
+        while (!(sb::try_wait(row_full, 0) && sb::try_wait(row_full, 1)) && sb::timer_ns() - t0 < 1000000ull) { }
+    }
+    __syncthreads();
+    if (ranks > 1) cluster_sync_all();
+}
+
 // ------------------------------------------------------------------------------------------ host side
 template <typename T, bool REST, int MODE>
 static cudaError_t distill_launch_as(const DistillParams& p, int cluster, size_t smem, cudaStream_t s) {
@@ -488,6 +885,58 @@ static cudaError_t distill_launch_as(const DistillParams& p, int cluster, size_t
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, distill_kernel<T, REST, MODE>, p);
 }
+// Clusters of the many-rows kernel that are resident at once.
+template <typename T, bool REST>
+static int rows_resident(int cluster, size_t smem) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    static std::atomic<bool> attr_set[64];    // zero-initialised; set-up is idempotent, so a race repeats it harmlessly
+    if (dev < 0 || dev >= 64 || !attr_set[dev]) {
+        if (cudaFuncSetAttribute(distill_rows_kernel<T, REST>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024) != cudaSuccess) {
+            (void)cudaGetLastError();
+            return 0;
+        }
+        if (dev >= 0 && dev < 64) attr_set[dev] = true;
+    }
+    return smem <= 110 * 1024 ? 2 * device_sm_count() / cluster : 0;
+}
+template <typename T, bool REST>
+static cudaError_t rows_launch(const DistillParams& p, int cluster, int clusters, size_t smem, cudaStream_t s) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.gridDim = dim3(static_cast<unsigned>(clusters) * cluster, 1, 1);
+    cfg.blockDim = dim3(kDsRowsThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = static_cast<unsigned>(cluster); attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, distill_rows_kernel<T, REST>, p);
+}
+// The many-rows kernel, where a row fits a cluster's registers and there are more rows than clusters at once (1 if not taken).
+template <typename T, bool REST>
+static int rows_try_as(const DistillParams& p, int cluster, cudaStream_t s) {
+    if (p.slice / DsType<T>::E + 1 > kDsThreads * kDsVecs) return 1;
+    const RowsSmem<T> lay(p.slice, p.k, p.mark_bytes);
+    const int clusters = rows_resident<T, REST>(cluster, static_cast<size_t>(lay.total));
+    if (clusters < 1 || p.M <= clusters) return 1;
+    SLIM_CUDA_TRY((rows_launch<T, REST>(p, cluster, clusters, static_cast<size_t>(lay.total), s)));
+    return SLIM_OK;
+}
+template <typename T>
+static int rows_try_rest(const DistillParams& p, int cluster, cudaStream_t s) {
+    return p.lse != nullptr ? rows_try_as<T, true>(p, cluster, s) : rows_try_as<T, false>(p, cluster, s);
+}
+static int rows_try(const DistillParams& p, int type, int cluster, cudaStream_t s) {
+    switch (type) {
+        case SLIM_F32: return rows_try_rest<float>(p, cluster, s);
+        case SLIM_F16: return rows_try_rest<__half>(p, cluster, s);
+        default: return rows_try_rest<__nv_bfloat16>(p, cluster, s);
+    }
+}
+
 template <typename T, int MODE>
 static cudaError_t distill_launch_rest(const DistillParams& p, int cluster, size_t smem, cudaStream_t s) {
     return p.lse != nullptr ? distill_launch_as<T, true, MODE>(p, cluster, smem, s) : distill_launch_as<T, false, MODE>(p, cluster, smem, s);
@@ -540,6 +989,10 @@ static int distill(int mode, const void* logits, int type, long long ld, const v
     p.mark_bytes = lse != nullptr ? (p.slice / E + 1 + 3) / 4 * 4 : 0;
     const size_t smem = static_cast<size_t>(entry_bytes(k)) + p.mark_bytes;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (mode == kDsStep) {
+        const int taken = rows_try(p, type, cluster, s);
+        if (taken <= 0) return taken;
+    }
     SLIM_CUDA_TRY(mode == kDsLoss ? distill_launch<kDsLoss>(p, type, cluster, smem, s)
                   : mode == kDsGrad ? distill_launch<kDsGrad>(p, type, cluster, smem, s) : distill_launch<kDsStep>(p, type, cluster, smem, s));
     return SLIM_OK;

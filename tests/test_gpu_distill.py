@@ -95,6 +95,38 @@ def test_rows_longer_than_a_cta_or_a_cluster_holds(M, V, kind, rest):
     _run_all(*_case(M, V, 33, kind, 1.0, rest, seed=V), 1.0, kind)
 
 
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("M,V,k", [(297, 1000, 5), (900, 333, 1), (450, 8191, 70), (310, 20003, 300), (200, 70001, 33)])
+def test_many_rows(M, V, k, kind, rest):
+    """More rows than CTAs, or clusters, at once; rows off 16 bytes; among them every kind of row that is not the ordinary one."""
+    student, index, value, lse, dloss = _case(M, V, k, kind, 1.0, rest, M + V)
+    index[3, :] = -1
+    student[3, :] = float("nan")
+    index[M - 1, :] = V
+    index[5, k // 2] = -1
+    if k > 2:
+        index[7, 2] = index[7, 0]
+        index[M - 2, :] = index[M - 2, 0]
+        if rest:
+            value[M - 2, :] -= 7.0
+    student[11, ::2] = -float("inf")
+    student[12, :] = -float("inf")
+    value[13, :] = -float("inf")
+    loss, grad = _run_all(student, index, value, lse, dloss, 1.0, kind)
+    assert (loss[[3, M - 1]] == 0).all() and (grad[[3, M - 1]] == 0).all()
+
+
+def test_not_finite_rows_among_many_stay_alone():
+    student, index, value, lse, dloss = _case(400, 5001, 6, "bf16", 1.0, True, 8)
+    student[1, 77] = float("nan")
+    student[399, 4001] = float("inf")
+    loss, grad = _slim().distill_step(student.cuda(), index.cuda(), value.cuda(), dloss.cuda(), teacher_lse=lse.cuda())
+    assert torch.isnan(loss[[1, 399]]).all() and torch.isnan(grad[[1, 399]]).all()
+    keep = [i for i in range(400) if i not in (1, 399)]
+    _check(student[keep], index[keep], value[keep], lse[keep], dloss[keep], 1.0, "bf16", loss[keep], grad[keep])
+
+
 @pytest.mark.parametrize("index_type", [torch.int32, torch.int64])
 @pytest.mark.parametrize("value_type", [torch.float16, torch.bfloat16, torch.float32])
 def test_types_of_the_entries(index_type, value_type):
@@ -181,7 +213,7 @@ def test_strided_rows(V, ld, off, ldg, offg, kind):
     assert torch.equal(before, out_wide)                       # nothing beside the rows was written
 
 
-@pytest.mark.parametrize("M,V", [(3, 1001), (2, 40000), (1, 150001), (300, 600)])
+@pytest.mark.parametrize("M,V", [(3, 1001), (2, 40000), (1, 150001), (300, 600), (700, 4001), (200, 70001)])
 @pytest.mark.parametrize("step", [False, True])
 def test_gradient_in_place_of_the_logits(M, V, step):
     slim = _slim()
