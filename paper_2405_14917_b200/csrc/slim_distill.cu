@@ -143,6 +143,36 @@ __device__ __forceinline__ float ex2(float v) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
+__device__ __forceinline__ float rcp(float v) {      // within an ulp
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// What a row's sums come to: R outside the set and z of the set's columns (all of it in R without the rest), and the teacher's listed
+// mass, that of the rest (0 without it) and both together.
+struct RowTerms {
+    float ref, R, Z, p_in;   // the row's maximum (0 if that is minus infinity); Z = R + z; the set's mass
+    float inv_z, factor;     // of 2^((s - ref) c) in the gradient of the columns outside the set, but for the row's weight
+};
+template <bool REST>
+__device__ __forceinline__ RowTerms row_terms(float m, float R, float z, float q_sum, float q_rest, float mass) {
+    RowTerms t;
+    t.ref = m == -INFINITY ? 0.f : m;
+    t.R = REST && R < 1.17549435e-38f ? 0.f : R;     // below fp32's normal range there is nothing
+    t.Z = t.R + z;
+    const float over = rcp(t.Z);
+    t.inv_z = t.Z == 0.f ? 0.f : over;
+    t.p_in = z * t.inv_z;
+    t.factor = mass * t.inv_z;
+    // p (1 - q'/p') = 2^.. (p' - q') / (p' Z), where p' is what the set leaves of 1, or R / Z where that would cancel
+    if (REST && !(q_rest == 0.f))
+        t.factor = t.Z == 0.f || t.R == 0.f ? 0.f : t.p_in < 0.5f ? (q_sum - t.p_in) * rcp(1.f - t.p_in) * over : (t.R * over - q_rest) * rcp(t.R);
+    return t;
+}
+// log p', in 64 bits.
+__device__ __forceinline__ double log_rest(const RowTerms& t, double log_z) {
+    return t.Z == 0.f || t.R == 0.f ? -INFINITY : t.p_in < 0.5f ? log1p(-static_cast<double>(t.p_in)) : log(static_cast<double>(t.R)) - log_z;
+}
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -353,40 +383,38 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
         if (ranks > 1) cluster_sync_all();           // grad may be logits: every CTA of the row has its entries' logits
     }
 
-    // ---- what the row comes to, by every warp for itself: Z, and the masses of the set and of the rest
-    const float ref = m == -INFINITY ? 0.f : m;
+    // ---- what the row comes to, by every warp for itself
     const double q_sum = s_row[0];
     const bool any = s_row[1] != 0.0;
-    double Z = R, p_rest = 0.0, q_rest = 0.0, p_in = 0.0;
-    bool little = false;                             // the set has less than half of the mass: the rest is what it leaves of 1
+    double q_rest = 0.0;
+    float z = 0.f;
     if (REST) {
-        double z = 0.0;
+        const float ref = m == -INFINITY ? 0.f : m;
         int columns = 0;
         for (int j = lane; j < p.k; j += 32)
             if (s_first[j]) { z += ex2((s_s[j] - ref) * p.c); ++columns; }
-        z = warp_sum(z);
-        Z += z;
-        p_in = Z == 0.0 ? 0.0 : z / Z;
-        little = p_in < 0.5;
-        p_rest = Z == 0.0 ? 0.0 : little ? 1.0 - p_in : R / Z;
-        q_rest = static_cast<int>(__reduce_add_sync(0xffffffffu, columns)) < p.V ? fmax(1.0 - q_sum, 0.0) : 0.0;
-        if (q_sum != q_sum) q_rest = q_sum;          // a NaN among the teacher's values
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        columns = static_cast<int>(__reduce_add_sync(0xffffffffu, columns));
+        if (columns < p.V) q_rest = q_sum >= 1.0 ? 0.0 : 1.0 - q_sum;         // NaN stays NaN
     }
+    const double mass = q_sum + q_rest;
+    const RowTerms t = row_terms<REST>(m, static_cast<float>(R), z, static_cast<float>(q_sum), static_cast<float>(q_rest), static_cast<float>(mass));
     // loss, in 64 bits, by the warp that is given it (below, beside the gradient)
     auto write_loss = [&] {
-        const double ln2 = 0.69314718055994530942, cd = p.c, lz = log(Z);
+        const double ln2 = 0.69314718055994530942, cd = p.c, lz = log(static_cast<double>(t.Z));
         double l = 0.0;
         for (int j = lane; j < p.k; j += 32) {
             const double q = s_q[j];
             if (s_idx[j] < 0 || q == 0.0) continue;
-            l += q * (s_lq[j] - (Z == 0.0 ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(ref)) * cd * ln2 - lz));
+            l += q * (s_lq[j] - (t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lz));
         }
         l = warp_sum(l);
-        if (REST && !(q_rest == 0.0)) l += q_rest * (log(q_rest) - (p_rest == 0.0 ? -INFINITY : little ? log1p(-p_in) : log(p_rest)));
+        if (REST && !(q_rest == 0.0)) l += q_rest * (log(q_rest) - log_rest(t, lz));
         if (lane == 0) {
             p.loss[row] = any ? static_cast<float>(l) : 0.f;
             if (MODE == kDsLoss && p.saved != nullptr)
-                *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) = make_float4(m, static_cast<float>(Z), static_cast<float>(R), 0.f);
+                *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) = make_float4(m, t.Z, t.R, 0.f);
         }
     };
     if (MODE == kDsLoss) {
@@ -396,19 +424,12 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     }
 
     // ---- the gradient: one factor for the whole row, then the listed columns
-    // Without a mass outside, or for the listed columns, p_v is multiplied by the teacher's whole mass; with one, that of the others is
-    // 1 - q'/p' = (p' - q') / p', and p' - q' = sum q - p_in where p' is what p_in leaves of 1.
     const double d = static_cast<double>(p.dloss[row]) * p.inv_t;
-    const float inv_z = Z == 0.0 ? 0.f : 1.f / static_cast<float>(Z);
-    const double mass = q_sum + q_rest;
-    float other = static_cast<float>(mass);
-    if (REST && !(q_rest == 0.0))
-        other = p_rest == 0.0 ? 0.f : static_cast<float>(little ? q_sum - p_in : p_rest - q_rest) / static_cast<float>(p_rest);
-    const float factor = any ? other * inv_z * static_cast<float>(d) : 0.f;
+    const float factor = any ? t.factor * static_cast<float>(d) : 0.f;
     T* r_grad = static_cast<T*>(p.grad) + static_cast<long long>(row) * p.ldg;
     T* g_base = r_grad + v0 - sl.shift;
     const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
-    const uint64_t neg2 = pair2(-ref, -ref), factor2 = pair2(factor, factor);
+    const uint64_t neg2 = pair2(-t.ref, -t.ref), factor2 = pair2(factor, factor);
     for (int j0 = 0; j0 < sl.nv; j0 += kDsVecs * kDsThreads) {
         if (MODE == kDsStep && sl.nv > kDsVecs * kDsThreads) {          // more than the registers hold: read again
 #pragma unroll
@@ -454,7 +475,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
             double q = s_q[j];
             if (twice)
                 for (int o = j + 1; o < p.k; ++o) q += s_idx[o] == i ? s_q[o] : 0.0;
-            r_grad[i] = DsType<T>::round(static_cast<float>((static_cast<double>(ex2((s_s[j] - ref) * p.c) * inv_z) * mass - q) * d));
+            r_grad[i] = DsType<T>::round(static_cast<float>((static_cast<double>(ex2((s_s[j] - t.ref) * p.c) * t.inv_z) * mass - q) * d));
         }
     }
     if (MODE == kDsStep) {
@@ -464,29 +485,41 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
 }
 
 // ------------------------------------------------------------------------------------------ the one pass over many rows
-// With more rows than CTAs at once, a CTA (or cluster) takes row after row, and what a row waits for is done for the next one meanwhile, by a seventeenth
-// warp: it has the row brought into shared memory (one bulk copy), reads the entries and the logits at them, works out the teacher's
-// probabilities and marks the listed columns; when the sixteen have the row's statistics it computes its loss beside their
-// gradient.  They take the row from shared memory into registers at once, which frees the buffer for the next.  4096 x 32000 bf16 took 173 us with
+// With more rows than CTAs at once, a CTA (or cluster) takes row after row, and what a row waits for is done for later ones meanwhile, by two warps beside
+// the sixteen that take the rows in turn: they have a row brought into shared memory (one bulk copy), read its entries and the logits at them two
+// rows ahead, work out the teacher's probabilities, mark the listed columns, and when the sixteen have the row's statistics compute its loss beside their
+// gradient.  (One such warp was what all waited for: it runs some 700 instructions per row, alone in its code and at an instruction in 20 cycles.)
+// The sixteen take the row from shared memory into registers at once, which frees the buffer for the next.  4096 x 32000 bf16 took 173 us with
 // a CTA per row (of 22000 cycles 9000 went until the entries were there and 4000 into the row's own terms), two per SM.
 // Statistics meet in a cluster by asynchronous stores that count on the receiver's barrier.  Every wait is bounded; rows left
 // undone by one that gives up have NaN for a loss.
-constexpr int kDsRowsThreads = kDsThreads + 32;
+constexpr int kDsRowsThreads = kDsThreads + 64;
 
-struct RowTerms {            // what a row comes to, for its loss
-    float ref;
-    double R, Z, p_in, q_rest, p_rest;
+struct RowTeacher {          // what its entries come to
+    double mass, q_rest, d;  // the teacher's whole mass, that outside the set; the row's weight over the temperature
+    float q_sum;             // the teacher's listed mass
+    float top, z;            // the student's largest logit of the set, its sum of 2^((s - top) c) over the set's columns
+    int any, twice;          // something to learn from; a column in two entries
 };
+// Slots of the table in which a row's columns are looked for: a power of two, at least twice as many as there are entries.
+__host__ __device__ __forceinline__ int table_slots(int k) {
+    int n = 32;
+    while (n < 2 * k) n *= 2;
+    return n;
+}
+
+constexpr int kDsEntryBufs = 4;
 
 template <typename T>
 struct RowsSmem {            // byte offsets
-    int row, entries, entry_stride, mark, total;
+    int row, table, entries, entry_stride, mark, total;
     __host__ __device__ RowsSmem(int slice, int k, int mark_bytes) {
         row = 0;
-        entries = (slice / DsType<T>::E + 1) * 16;
+        table = (slice / DsType<T>::E + 1) * 16;
+        entries = table + 2 * 4 * table_slots(k);      // one for each of the two warps
         mark = entry_bytes(k);
         entry_stride = mark + (mark_bytes + 15) / 16 * 16;
-        total = entries + 2 * entry_stride;
+        total = entries + kDsEntryBufs * entry_stride;
     }
 };
 
@@ -510,20 +543,19 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
     constexpr int E = DsType<T>::E;
     extern __shared__ __align__(16) unsigned char ds_smem[];
     const RowsSmem<T> lay(p.slice, p.k, p.mark_bytes);
-    __shared__ __align__(8) uint64_t s_bar[10];
+    __shared__ __align__(8) uint64_t s_bar[2 + 3 * kDsEntryBufs + 2];
     __shared__ float2 s_part[2][kDsWarps];
     __shared__ float2 s_slice[2][kDsMaxCluster];
-    __shared__ double s_teacher[2][2];                                 // the teacher's listed mass; whether there is any
-    __shared__ int s_twice[2];
-    __shared__ RowTerms s_terms[2];
+    __shared__ RowTeacher s_teacher[kDsEntryBufs];
+    __shared__ RowTerms s_terms[kDsEntryBufs];
     __shared__ int s_abort;
     volatile int* abort = &s_abort;
     const uint32_t bar0 = smem_u32(s_bar);
     const uint32_t row_full = bar0, row_empty = bar0 + 8;
     auto ent_full = [&](int b) { return bar0 + 16u + 8u * b; };
-    auto ent_empty = [&](int b) { return bar0 + 32u + 8u * b; };
-    auto terms_full = [&](int b) { return bar0 + 48u + 8u * b; };
-    auto slice_full = [&](int b) { return bar0 + 64u + 8u * b; };
+    auto ent_empty = [&](int b) { return bar0 + 16u + 8u * (kDsEntryBufs + b); };
+    auto terms_full = [&](int b) { return bar0 + 16u + 8u * (2 * kDsEntryBufs + b); };
+    auto slice_full = [&](int b) { return bar0 + 16u + 8u * (3 * kDsEntryBufs + b); };
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ranks = p.ranks, rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
@@ -533,12 +565,12 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
         s_abort = 0;
         sb::init(row_full, 1);
         sb::init(row_empty, kDsWarps);
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kDsEntryBufs; ++b) {
             sb::init(ent_full(b), 1);
             sb::init(ent_empty(b), kDsWarps);
             sb::init(terms_full(b), 1);
-            sb::init(slice_full(b), 1);
         }
+        for (int b = 0; b < 2; ++b) sb::init(slice_full(b), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
@@ -547,10 +579,51 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
     auto slice_of = [&](int row) { return Slice<T>(logits + static_cast<long long>(row) * p.ld + v0, v1 - v0); };
     const double ln2 = 0.69314718055994530942, cd = p.c;
 
-    if (warp == kDsWarps) {
-        // ------------------------------------------------------------------ the seventeenth warp
-        auto entries = [&](int row, int n) {           // of the n-th row of this CTA; its buffers are free
-            const int b = n & 1;
+    if (warp >= kDsWarps) {
+        // ------------------------------------------------------------------ the two beside them: even rows and odd rows of this CTA
+        // The columns and values of a row's first 64 entries, its log-sum-exp and its weight are on their way while the row before is prepared, as
+        // they lie in memory: a load takes some 5000 cycles beside the rows' traffic, and a conversion here would wait for it.
+        const int turn = warp - kDsWarps;
+        constexpr int AHEAD = 2;
+        int2 f_idx[AHEAD];
+        uint32_t f_val[AHEAD];
+        float f_lse = 0.f, f_weight = 0.f;
+        const int slots = table_slots(p.k);
+        int* table = reinterpret_cast<int*>(ds_smem + lay.table) + turn * slots;
+        auto raw_index = [&](size_t at) {
+            if (p.index64) return static_cast<const int2*>(p.index)[at];
+            return make_int2(static_cast<const int*>(p.index)[at], 0);
+        };
+        auto column = [&](int2 raw) {                  // -1: absent
+            const bool in = (!p.index64 || raw.y == 0) && raw.x >= 0 && raw.x < p.V;
+            return in ? raw.x : -1;
+        };
+        auto raw_value = [&](size_t at) -> uint32_t {
+            if (p.value_type == SLIM_F32) return static_cast<const uint32_t*>(p.value)[at];
+            return static_cast<const unsigned short*>(p.value)[at];
+        };
+        auto teacher_logit = [&](uint32_t raw) {
+            if (p.value_type == SLIM_F32) return __uint_as_float(raw);
+            if (p.value_type == SLIM_F16) return __half2float(__ushort_as_half(static_cast<unsigned short>(raw)));
+            return __uint_as_float(raw << 16);
+        };
+        auto fetch = [&](int row) {
+            if (row >= p.M) return;
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (32 * u >= p.k) break;
+                const int j = lane + 32 * u;
+                const size_t at = static_cast<size_t>(row) * p.k + j;
+                if (j < p.k) {
+                    f_idx[u] = raw_index(at);
+                    f_val[u] = raw_value(at);
+                }
+            }
+            if (REST) f_lse = p.lse[row];
+            f_weight = p.dloss[row];
+        };
+        auto entries = [&](int row, int n) {           // of the n-th row of this CTA; its buffer is free, its first entries fetched
+            const int b = n % kDsEntryBufs;
             unsigned char* e0 = ds_smem + lay.entries + b * lay.entry_stride;
             double* s_q = reinterpret_cast<double*>(e0);
             double* s_lq = s_q + p.k;
@@ -560,58 +633,84 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             uint32_t* s_mark = reinterpret_cast<uint32_t*>(e0 + lay.mark);
             const T* r_logits = logits + static_cast<long long>(row) * p.ld;
             const Slice<T> sl = slice_of(row);
-            // what of the slice is not whole vectors
-            if (lane < 2 * E) {
-                const int j = lane < E ? 0 : sl.nv - 1, i = j * E + lane % E;
-                if (sl.nv > 0 && !sl.whole(j))
-                    reinterpret_cast<T*>(ds_smem + lay.row)[i] = i >= sl.shift && i < sl.end ? sl.base[i] : DsType<T>::round(-INFINITY);
+            T g[AHEAD];
+            int r_idx[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                r_idx[u] = lane + 32 * u < p.k ? column(f_idx[u]) : -1;
+                if (r_idx[u] >= 0) g[u] = r_logits[r_idx[u]];
             }
-            double top = -INFINITY;
-            int any = 0, finite = 0, twice = 0;
-            for (int j = lane; j < p.k; j += 32) {
-                const size_t at = static_cast<size_t>(row) * p.k + j;
-                const long long i = p.index64 ? static_cast<const long long*>(p.index)[at] : static_cast<const int*>(p.index)[at];
-                const bool in = i >= 0 && i < p.V;
-                double u;
-                if (p.value_type == SLIM_F32) u = static_cast<const float*>(p.value)[at];
-                else if (p.value_type == SLIM_F16) u = __half2float(static_cast<const __half*>(p.value)[at]);
-                else u = __bfloat162float(static_cast<const __nv_bfloat16*>(p.value)[at]);
-                u *= p.inv_t;
-                s_idx[j] = in ? static_cast<int>(i) : -1;
-                s_s[j] = in ? DsType<T>::one(r_logits[i]) : 0.f;
-                s_lq[j] = u;
-                if (in) { top = fmax(top, u); any = 1; finite |= !(u == -INFINITY); }
-            }
-            if (lane < 4) s_idx[p.k + lane] = -1;
+            for (int j = lane; j < slots / 4; j += 32) reinterpret_cast<int4*>(table)[j] = make_int4(-1, -1, -1, -1);
             if (REST)
-                for (int j = lane; j < p.mark_bytes / 4; j += 32) s_mark[j] = 0u;
+                for (int j = lane; j < (p.mark_bytes + 15) / 16; j += 32) reinterpret_cast<uint4*>(s_mark)[j] = make_uint4(0, 0, 0, 0);
+            if (lane < 4) s_idx[p.k + lane] = -1;
             __syncwarp();
-            for (int j = lane; j < p.k; j += 32) {
-                const int i = s_idx[j];
-                bool again = false;
-                for (int o = 0; o < j; o += 4) {
-                    const int4 c = *reinterpret_cast<const int4*>(s_idx + o);
-                    again = again || (c.x == i) || (o + 1 < j && c.y == i) || (o + 2 < j && c.z == i) || (o + 3 < j && c.w == i);
+            double top = -INFINITY;
+            int any = 0, finite = 0, twice = 0, columns = 0;
+            auto take = [&](int j, int i, float value) {
+                const double u = static_cast<double>(value) * p.inv_t;
+                s_idx[j] = i;
+                s_lq[j] = u;
+                s_first[j] = i >= 0;
+                if (i >= 0) {
+                    any = 1;
+                    ++columns;
+                    if (!REST) { top = fmax(top, u); finite |= !(u == -INFINITY); }
+                    // is the column there already?  A table with open slots; entries that lose a slot to another look at the next
+                    int at = static_cast<int>(static_cast<uint32_t>(i) * 2654435769u >> 8) & (slots - 1);
+                    for (;;) {
+                        const int was = atomicCAS(table + at, -1, i);
+                        if (was == -1) break;
+                        if (was == i) { twice = 1; break; }
+                        at = (at + 1) & (slots - 1);
+                    }
+                    if (REST && i >= v0 && i < v1) {
+                        const int e = i - v0 + sl.shift;
+                        atomicOr(s_mark + (e / E >> 2), 1u << ((e / E & 3) * 8 + e % E));
+                    }
                 }
-                s_first[j] = i >= 0 && !again;
-                twice |= i >= 0 && again;
-                if (REST && i >= v0 && i < v1) {
-                    const int e = i - v0 + sl.shift;
-                    atomicOr(s_mark + (e / E >> 2), 1u << ((e / E & 3) * 8 + e % E));
+            };
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (32 * u >= p.k) break;
+                const int j = lane + 32 * u;
+                if (j < p.k) take(j, r_idx[u], teacher_logit(f_val[u]));
+            }
+            const float lse = f_lse, weight = f_weight;
+            fetch(row + 2 * stride);
+#pragma unroll 1
+            for (int j = lane + 32 * AHEAD; j < p.k; j += 32) {
+                const size_t at = static_cast<size_t>(row) * p.k + j;
+                const int i = column(raw_index(at));
+                take(j, i, teacher_logit(raw_value(at)));
+                s_s[j] = i >= 0 ? DsType<T>::one(r_logits[i]) : 0.f;
+            }
+            __syncwarp();
+            any = __any_sync(0xffffffffu, any);
+            if (__any_sync(0xffffffffu, twice)) {      // which entry is its column's first: the one with the lowest number
+                twice = 1;
+                columns = 0;
+                for (int j = lane; j < p.k; j += 32) {
+                    const int i = s_idx[j];
+                    bool again = i < 0;
+                    for (int o = 0; o < j; ++o) again = again || s_idx[o] == i;
+                    s_first[j] = !again;
+                    columns += !again;
                 }
             }
-            any = __any_sync(0xffffffffu, any);
             double norm;
-            if (REST) norm = p.lse[row];
+            if (REST) norm = lse;
             else {
                 any = __any_sync(0xffffffffu, finite);
                 top = warp_max(top);
                 double sum = 0.0;
+#pragma unroll 1
                 for (int j = lane; j < p.k; j += 32)
                     if (s_idx[j] >= 0) sum += exp(s_lq[j] - top);
                 norm = top + log(warp_sum(sum));
             }
             double q_sum = 0.0;
+#pragma unroll 1
             for (int j = lane; j < p.k; j += 32) {
                 const double lq = s_lq[j] - norm;
                 const double q = s_idx[j] >= 0 && any ? exp(lq) : 0.0;
@@ -620,13 +719,43 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                 q_sum += q;
             }
             q_sum = warp_sum(q_sum);
-            twice = __any_sync(0xffffffffu, twice);
-            if (lane == 0) { s_teacher[b][0] = q_sum; s_teacher[b][1] = any; s_twice[b] = twice; }
+            columns = static_cast<int>(__reduce_add_sync(0xffffffffu, columns));
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (lane + 32 * u < p.k) s_s[lane + 32 * u] = r_idx[u] >= 0 ? DsType<T>::one(g[u]) : 0.f;
+            float s_top = -INFINITY, z = 0.f;
+            if (REST) {
+#pragma unroll 1
+                for (int j = lane; j < p.k; j += 32)
+                    if (s_idx[j] >= 0) s_top = fmaxf(s_top, s_s[j]);
+                s_top = redux_max(s_top);
+                const float r = s_top == -INFINITY ? 0.f : s_top;
+#pragma unroll 1
+                for (int j = lane; j < p.k; j += 32)
+                    if (s_first[j]) z += ex2((s_s[j] - r) * p.c);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+            }
+            if (lane == 0) {
+                RowTeacher t;
+                t.q_rest = REST && columns < p.V ? (q_sum >= 1.0 ? 0.0 : 1.0 - q_sum) : 0.0;       // NaN stays NaN
+                t.mass = q_sum + t.q_rest;
+                t.d = static_cast<double>(weight) * p.inv_t;
+                t.q_sum = static_cast<float>(q_sum);
+                t.top = s_top; t.z = z; t.any = any; t.twice = twice;
+                s_teacher[b] = t;
+            }
             __syncwarp();
             if (lane == 0) sb::arrive(ent_full(b));
         };
-        auto bring = [&](int row) {                    // the whole vectors of the slice
+        // The slice into shared memory, whose buffer is free: the whole vectors by a bulk copy, the ends as they are, minus infinity beside them.
+        auto bring = [&](int row) {
             const Slice<T> sl = slice_of(row);
+            const int j = lane < E ? 0 : sl.nv - 1, i = j * E + lane % E;
+            if (lane < 2 * E && sl.nv > 0 && !sl.whole(j))
+                reinterpret_cast<T*>(ds_smem + lay.row)[i] = i >= sl.shift && i < sl.end ? sl.base[i] : DsType<T>::round(-INFINITY);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the buffer was read, and its ends are written, by ordinary accesses
+            __syncwarp();
             const int from = sl.shift > 0 ? 1 : 0, to = sl.end / E;
             const uint32_t bytes = to > from ? 16u * static_cast<uint32_t>(to - from) : 0u;
             if (lane == 0) {
@@ -635,44 +764,49 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             }
             __syncwarp();
         };
-        int n = 0;
-        if (first < p.M) { bring(first); entries(first, 0); }
-        for (int row = first; row < p.M; row += stride, ++n) {
-            const int b = n & 1, next = row + stride;
+        int n = turn;
+        int row = first + turn * stride;
+        if (row < p.M) {
+            if (n == 0) bring(row);
+            fetch(row);
+            entries(row, n);
+        }
+        for (; row < p.M; row += 2 * stride, n += 2) {
+            const int b = n % kDsEntryBufs;
             bool ok = true;
-            if (next < p.M) {
-                ok = __all_sync(0xffffffffu, sb::wait(row_empty, n & 1u, abort));
-                if (ok) {
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the buffer was read, and its ends written, by ordinary accesses
-                    bring(next);
-                    if (n > 0) ok = __all_sync(0xffffffffu, sb::wait(ent_empty(b ^ 1), ((n - 1) >> 1) & 1u, abort));
-                }
-                if (ok) entries(next, n + 1);
+            if (n > 0) {                               // the buffer is free when the sixteen have taken the row before
+                ok = __all_sync(0xffffffffu, sb::wait(row_empty, (n - 1) & 1u, abort));
+                if (ok) bring(row);
             }
-            ok = ok && __all_sync(0xffffffffu, sb::wait(terms_full(b), (n >> 1) & 1u, abort));
+            if (ok && row + 2 * stride < p.M) {
+                if (n >= 2) ok = __all_sync(0xffffffffu, sb::wait(ent_empty((n + 2) % kDsEntryBufs), ((n - 2) / kDsEntryBufs) & 1u, abort));
+                if (ok) entries(row + 2 * stride, n + 2);
+            }
+            ok = ok && __all_sync(0xffffffffu, sb::wait(terms_full(b), (n / kDsEntryBufs) & 1u, abort));
             if (!ok) {
-                for (int r = row; r < p.M && rank == 0; r += stride)
-                    if (lane == 0) p.loss[r] = NAN;
+                for (int r = row; r < p.M && rank == 0 && lane == 0; r += 2 * stride) p.loss[r] = NAN;
                 break;
             }
-            if (rank != 0) continue;
-            const RowTerms t = s_terms[b];
-            unsigned char* e0 = ds_smem + lay.entries + b * lay.entry_stride;
-            const double* s_q = reinterpret_cast<const double*>(e0);
-            const double* s_lq = s_q + p.k;
-            const int* s_idx = reinterpret_cast<const int*>(s_lq + p.k);
-            const float* s_s = reinterpret_cast<const float*>(s_idx + p.k + 4);
-            const double lz = log(t.Z);
-            double l = 0.0;
-            for (int j = lane; j < p.k; j += 32) {
-                const double q = s_q[j];
-                if (s_idx[j] < 0 || q == 0.0) continue;
-                l += q * (s_lq[j] - (t.Z == 0.0 ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lz));
+            if (rank == 0) {
+                const RowTerms t = s_terms[b];
+                const RowTeacher te = s_teacher[b];
+                const double* s_q = reinterpret_cast<const double*>(ds_smem + lay.entries + b * lay.entry_stride);
+                const double* s_lq = s_q + p.k;
+                const int* s_idx = reinterpret_cast<const int*>(s_lq + p.k);
+                const float* s_s = reinterpret_cast<const float*>(s_idx + p.k + 4);
+                const double lz = log(static_cast<double>(t.Z));
+                double l = 0.0;
+#pragma unroll 1
+                for (int j = lane; j < p.k; j += 32) {
+                    const double q = s_q[j];
+                    if (s_idx[j] < 0 || q == 0.0) continue;
+                    l += q * (s_lq[j] - (t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lz));
+                }
+                l = warp_sum(l);
+                if (REST && !(te.q_rest == 0.0)) l += te.q_rest * (log(te.q_rest) - log_rest(t, lz));
+                if (lane == 0) p.loss[row] = te.any ? static_cast<float>(l) : 0.f;
             }
-            l = warp_sum(l);
-            if (REST && !(t.q_rest == 0.0))
-                l += t.q_rest * (log(t.q_rest) - (t.p_rest == 0.0 ? -INFINITY : t.p_in < 0.5 ? log1p(-t.p_in) : log(t.p_rest)));
-            if (lane == 0) p.loss[row] = s_teacher[b][1] != 0.0 ? static_cast<float>(l) : 0.f;
+            __syncwarp();
         }
     } else {
         // ------------------------------------------------------------------ the sixteen
@@ -680,18 +814,17 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
         auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(kDsThreads) : "memory"); };
         int n = 0;
         for (int row = first; row < p.M; row += stride, ++n) {
-            const int b = n & 1;
-            const uint32_t ph = (n >> 1) & 1u;
-            const unsigned char* e0 = ds_smem + lay.entries + b * lay.entry_stride;
+            const int b = n & 1, eb = n % kDsEntryBufs;
+            const uint32_t ph = (n >> 1) & 1u, eph = (n / kDsEntryBufs) & 1u;
+            const unsigned char* e0 = ds_smem + lay.entries + eb * lay.entry_stride;
             const double* s_q = reinterpret_cast<const double*>(e0);
             const int* s_idx = reinterpret_cast<const int*>(s_q + 2 * p.k);
             const float* s_s = reinterpret_cast<const float*>(s_idx + p.k + 4);
             const uint8_t* s_first = reinterpret_cast<const uint8_t*>(s_s + p.k);
             const uint8_t* mark = e0 + lay.mark;
             const Slice<T> sl = slice_of(row);
-            const float weight = p.dloss[row];
             // a warp that gives up says so to the others at the next meeting; all leave there
-            bool ok = sb::wait(ent_full(b), ph, abort);
+            bool ok = sb::wait(ent_full(eb), eph, abort);
             ok = sb::wait(row_full, n & 1u, abort) && ok;
             __syncwarp();
             const uint4* buf = reinterpret_cast<const uint4*>(ds_smem + lay.row) + tid;
@@ -748,64 +881,39 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
             if (lane == 0) s_part[b][warp] = make_float2(tm, ws);
             meet();
-            float m;
-            double R;
-            auto join = [&](float2 part, bool in) {
+            float m, R;
+            auto join = [&](float2 part, bool in) {    // sixteen at most, in the low and the high half of the warp alike
                 m = redux_max(in ? part.x : -INFINITY);
-                double v = !in ? 0.0 : part.x == -INFINITY ? static_cast<double>(part.y) : static_cast<double>(part.y * ex2((part.x - m) * p.c));
+                R = !in ? 0.f : part.x == -INFINITY ? part.y : part.y * ex2((part.x - m) * p.c);
 #pragma unroll
-                for (int o = kDsWarps / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);       // in the low and the high half of the warp alike
-                R = __shfl_sync(0xffffffffu, v, 0);
+                for (int o = kDsWarps / 2; o > 0; o >>= 1) R += __shfl_xor_sync(0xffffffffu, R, o);
             };
-            join(s_part[b][lane % kDsWarps], lane < kDsWarps);
+            join(s_part[b][lane % kDsWarps], true);
             if (ranks > 1) {
                 if (tid == 0) sb::expect_tx(slice_full(b), 8u * ranks);
                 if (tid < ranks)
-                    st_async_f32x2(map_cluster(smem_u32(&s_slice[b][rank]), tid), make_float2(m, static_cast<float>(R)), map_cluster(slice_full(b), tid));
+                    st_async_f32x2(map_cluster(smem_u32(&s_slice[b][rank]), tid), make_float2(m, R), map_cluster(slice_full(b), tid));
                 ok = sb::wait(slice_full(b), ph, abort) && ok;
                 __syncwarp();
-                join(s_slice[b][lane % ranks], lane < ranks);
+                join(s_slice[b][lane % ranks], lane % kDsWarps < ranks);
             }
 
-            // ---- what the row comes to, by every warp for itself
-            const float ref = m == -INFINITY ? 0.f : m;
-            const double q_sum = s_teacher[b][0];
-            const bool any = s_teacher[b][1] != 0.0;
-            double Z = R, p_rest = 0.0, q_rest = 0.0;
-            float p_in = 0.f;
-            bool little = false;                       // the set has less than half of the mass: the rest is what it leaves of 1
-            if (REST) {
-                float z = 0.f;
-                int columns = 0;
-                for (int j = lane; j < p.k; j += 32)
-                    if (s_first[j]) { z += ex2((s_s[j] - ref) * p.c); ++columns; }
-                const double zd = warp_sum(static_cast<double>(z));
-                Z += zd;
-                p_in = Z == 0.0 ? 0.f : static_cast<float>(zd) / static_cast<float>(Z);
-                little = p_in < 0.5f;
-                p_rest = Z == 0.0 ? 0.0 : little ? 1.0 - static_cast<double>(p_in) : static_cast<double>(static_cast<float>(R) / static_cast<float>(Z));
-                q_rest = static_cast<int>(__reduce_add_sync(0xffffffffu, columns)) < p.V ? fmax(1.0 - q_sum, 0.0) : 0.0;
-                if (q_sum != q_sum) q_rest = q_sum;    // a NaN among the teacher's values
-            }
+            // ---- what the row comes to, by every thread for itself
+            const RowTeacher te = s_teacher[eb];
+            const float z = !REST ? 0.f : te.top == -INFINITY ? te.z : te.z * ex2((te.top - m) * p.c);
+            const RowTerms t = row_terms<REST>(m, R, z, te.q_sum, static_cast<float>(te.q_rest), static_cast<float>(te.mass));
             if (tid == 0) {
-                RowTerms t;
-                t.ref = ref; t.R = R; t.Z = Z; t.p_in = p_in; t.q_rest = q_rest; t.p_rest = p_rest;
-                s_terms[b] = t;
-                sb::arrive(terms_full(b));
+                s_terms[eb] = t;
+                sb::arrive(terms_full(eb));
             }
-            const double d = static_cast<double>(weight) * p.inv_t;
-            const float inv_z = Z == 0.0 ? 0.f : 1.f / static_cast<float>(Z);
-            const double mass = q_sum + q_rest;
-            float other = static_cast<float>(mass);
-            if (REST && !(q_rest == 0.0))
-                other = p_rest == 0.0 ? 0.f : static_cast<float>(little ? q_sum - static_cast<double>(p_in) : p_rest - q_rest) / static_cast<float>(p_rest);
-            const float factor = any ? other * inv_z * static_cast<float>(d) : 0.f;
+            const bool any = te.any != 0;
+            const float factor = any ? t.factor * static_cast<float>(te.d) : 0.f;
 
             // ---- the gradient: one factor for the whole row, then the listed columns
             T* r_grad = static_cast<T*>(p.grad) + static_cast<long long>(row) * p.ldg;
             T* g_base = r_grad + v0 - sl.shift;
             const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
-            const uint64_t neg2 = pair2(-ref, -ref), factor2 = pair2(factor, factor);
+            const uint64_t neg2 = pair2(-t.ref, -t.ref), factor2 = pair2(factor, factor);
 #pragma unroll
             for (int u = 0; u < kDsVecs; ++u) {
                 forget(x[u]);
@@ -841,13 +949,13 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                     const int i = s_idx[j];
                     if (!s_first[j] || i < v0 || i >= v1) continue;
                     double q = s_q[j];
-                    if (s_twice[b])
+                    if (te.twice)
                         for (int o = j + 1; o < p.k; ++o) q += s_idx[o] == i ? s_q[o] : 0.0;
-                    r_grad[i] = DsType<T>::round(static_cast<float>((static_cast<double>(ex2((s_s[j] - ref) * p.c) * inv_z) * mass - q) * d));
+                    r_grad[i] = DsType<T>::round(static_cast<float>((static_cast<double>(ex2((s_s[j] - t.ref) * p.c) * t.inv_z) * te.mass - q) * te.d));
                 }
             }
             __syncwarp();
-            if (lane == 0) sb::arrive(ent_empty(b));
+            if (lane == 0) sb::arrive(ent_empty(eb));
             if (gave_up) break;
         }
     }

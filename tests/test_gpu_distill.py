@@ -29,8 +29,9 @@ def _bounds(student, parts, grad_ref, dloss, T, kind):
     """Error bounds of the loss and of every gradient element.
 
     A log-probability carries, in units of 1: the rounding of log2(e)/T, of s - m and of their product (2^-24 each of D =
-    (m - s) log2(e)/T, at the column and, weighted, in the sum), ex2 (2^-22), and fp32 sums of at most 8 + 8 terms per 64 columns of a
-    thread (16 * 2^-24 for each of the passes over them); fp64 from there on.  D is cut at 150: beyond, p is 0 in fp32."""
+    (m - s) log2(e)/T, at the column and, weighted, in the sum), ex2 (2^-22, and again where a partial sum is brought to the row's maximum: three
+    times at most), and fp32 sums of positive terms: chains of at most 32 + 1 additions in a thread per pass, 5 in its warp, 4 over the warps, 3 over a
+    cluster and 32 + 5 over the entries, 2^-24 each; 1/Z within 2^-23.  The rest is fp64.  D is cut at 150: beyond, p is 0 in fp32."""
     s = student.double().numpy()
     finite = np.where(np.isfinite(s), s, -np.inf)
     with np.errstate(invalid="ignore"):
@@ -39,7 +40,7 @@ def _bounds(student, parts, grad_ref, dloss, T, kind):
     # in the sum an element of distance D weighs 2^-D, and D 2^-D < 0.54: the columns of a row add up to less than 0.54 V / Z of it, and Z >= 1
     p = parts["p"]
     in_sum = (p * D).sum(1)
-    d_sum = 2.0 ** -20 * passes + 2.0 ** -21 + 4 * 2.0 ** -24 * in_sum
+    d_sum = (33 * passes + 49) * 2.0 ** -24 + 3 * 2.0 ** -22 + 2.0 ** -23 + 4 * 2.0 ** -24 * in_sum
     d_col = d_sum[:, None] + 4 * 2.0 ** -24 * D + 2.0 ** -22
     q, q_rest, p_rest = parts["q"], parts["q_rest"], parts["p_rest"]
     ratio = np.divide(q_rest, p_rest, out=np.zeros_like(q_rest), where=p_rest > 0)
