@@ -459,9 +459,10 @@ int slim_fp8_linear(const void* x, int x_type, long long ldx, const void* codes,
  *   index   int32 or int64 (index_bytes 4 or 8) [M][k]; value [M][k] of any of the three types; teacher_lse, dloss, loss fp32 [M]
  *   saved   fp32 [M][4], 16-byte aligned: what _grad needs of _loss (same logits, entries, teacher_lse and temperature); may be NULL in _loss
  *   grad    [M][V] of the logits' type, row stride ldg >= V; may be the logits themselves (same pointer and stride)
- * _step is _loss and _grad in one pass: it reads the logits once (V up to 262144, 131072 for fp32; beyond, twice).  Sums
- * over the columns in fp32 and fp64, what is computed per entry in fp64; deterministic.  1 <= k <= SLIM_DISTILL_MAX_K,
- * V <= SLIM_DISTILL_MAX_V, temperature > 0. */
+ * _step is _loss and _grad in one call: rows up to 65000 columns (half as many of fp32) are read once, longer ones a second
+ * time, from L2 as a rule.  Sums over the columns in fp32, what is computed per entry in fp64; deterministic.
+ * 1 <= k <= SLIM_DISTILL_MAX_K, V <= SLIM_DISTILL_MAX_V, temperature > 0.  A device-side wait of the many-rows kernels that gives up leaves NaN
+ * in the losses of the rows left undone. */
 #define SLIM_DISTILL_MAX_K 1024
 #define SLIM_DISTILL_MAX_V 2097152
 int slim_distill_loss(const void* logits, int type, long long ld, const void* index, int index_bytes, const void* value, int value_type,

@@ -98,25 +98,26 @@ template <> struct DsType<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 round(float v) { return __float2bfloat16_rn(v); }
 };
 
-// Largest of a thread's vectors, two elements at a time where they are 16 bits wide (a NaN loses: it shows in the sum).
-__device__ __forceinline__ float vec_max(const uint4* x, int n, const float*) {
+// Largest of n of a thread's vectors, two elements at a time where they are 16 bits wide (a NaN loses: it shows in the sum).
+template <int n>
+__device__ __forceinline__ float vec_max(const uint4* x, const float*) {
     float m = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kDsVecs; ++u)
+    for (int u = 0; u < n; ++u)
         m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(x[u].x), __uint_as_float(x[u].y)), fmaxf(__uint_as_float(x[u].z), __uint_as_float(x[u].w))));
     return m;
 }
-template <typename H2, typename T>
+template <int n, typename H2, typename T>
 __device__ __forceinline__ float vec_max2(const uint4* x, T) {
     auto h = [](const uint32_t& w) { return *reinterpret_cast<const H2*>(&w); };
     H2 m = h(x[0].x);
 #pragma unroll
-    for (int u = 0; u < kDsVecs; ++u) m = __hmax2(m, __hmax2(__hmax2(h(x[u].x), h(x[u].y)), __hmax2(h(x[u].z), h(x[u].w))));
+    for (int u = 0; u < n; ++u) m = __hmax2(m, __hmax2(__hmax2(h(x[u].x), h(x[u].y)), __hmax2(h(x[u].z), h(x[u].w))));
     const float a = DsType<T>::one(m.x), b = DsType<T>::one(m.y);
     return fmaxf(fmaxf(a, b), -INFINITY);
 }
-__device__ __forceinline__ float vec_max(const uint4* x, int, const __half*) { return vec_max2<__half2>(x, __half()); }
-__device__ __forceinline__ float vec_max(const uint4* x, int, const __nv_bfloat16*) { return vec_max2<__nv_bfloat162>(x, __nv_bfloat16()); }
+template <int n> __device__ __forceinline__ float vec_max(const uint4* x, const __half*) { return vec_max2<n, __half2>(x, __half()); }
+template <int n> __device__ __forceinline__ float vec_max(const uint4* x, const __nv_bfloat16*) { return vec_max2<n, __nv_bfloat162>(x, __nv_bfloat16()); }
 
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ uint64_t pair2(float a, float b) {
@@ -169,9 +170,34 @@ __device__ __forceinline__ RowTerms row_terms(float m, float R, float z, float q
         t.factor = t.Z == 0.f || t.R == 0.f ? 0.f : t.p_in < 0.5f ? (q_sum - t.p_in) * rcp(1.f - t.p_in) * over : (t.R * over - q_rest) * rcp(t.R);
     return t;
 }
-// log p', in 64 bits.
-__device__ __forceinline__ double log_rest(const RowTerms& t, double log_z) {
-    return t.Z == 0.f || t.R == 0.f ? -INFINITY : t.p_in < 0.5f ? log1p(-static_cast<double>(t.p_in)) : log(static_cast<double>(t.R)) - log_z;
+// e^x in 64 bits for x up to a few (a log-probability), within 1e-14 of its value: x = n ln 2 + r after Cody and Waite (ln 2 = 355 / 512 and a
+// rest, so that n times the first is exact), Taylor's series of e^r to the eleventh power (|r| < 0.35: 0.35^12 / 12! < 1e-14) summed in pairs,
+// times 2^n.  Half as many dependent steps as a general exp(), which takes what lies beyond.
+__device__ __forceinline__ double exp_log(double x) {
+    if (x > 80.0) return exp(x);
+    if (x < -700.0) return 0.0;
+    const double n = rint(x * 1.44269504088896340736);
+    double r = fma(n, -355.0 / 512, x);
+    r = fma(n, 2.12194440054690582768e-4, r);
+    const double r2 = r * r, r4 = r2 * r2;
+    const double a = fma(r, 1.0, 1.0), b = fma(r, 1.0 / 6, 1.0 / 2), c = fma(r, 1.0 / 120, 1.0 / 24), d = fma(r, 1.0 / 5040, 1.0 / 720),
+                 e = fma(r, 1.0 / 362880, 1.0 / 40320), f = fma(r, 1.0 / 39916800, 1.0 / 3628800);
+    const double ab = fma(b, r2, a), cd = fma(d, r2, c), ef = fma(f, r2, e);
+    const double y = fma(fma(ef, r4, cd), r4, ab);
+    return __hiloint2double(__double2hiint(y) + (static_cast<int>(n) << 20), __double2loint(y));
+}
+// The logarithms that a loss needs, in 64 bits, by a lane each: of Z, q' and p' (what p_in leaves of 1, or R / Z where that would cancel).
+struct RowLogs {
+    double z, q_rest, p_rest;
+};
+__device__ __forceinline__ RowLogs row_logs(const RowTerms& t, double q_rest, int lane) {
+    const double v = log(lane == 0 ? static_cast<double>(t.Z) : lane == 1 ? q_rest : lane == 2 ? 1.0 - static_cast<double>(t.p_in) : static_cast<double>(t.R));
+    RowLogs l;
+    l.z = __shfl_sync(0xffffffffu, v, 0);
+    l.q_rest = __shfl_sync(0xffffffffu, v, 1);
+    const double left = __shfl_sync(0xffffffffu, v, 2), r = __shfl_sync(0xffffffffu, v, 3);
+    l.p_rest = t.Z == 0.f || t.R == 0.f ? -INFINITY : t.p_in < 0.5f ? left : r - l.z;
+    return l;
 }
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
@@ -202,9 +228,13 @@ struct Slice {
         return j * E >= shift && (j + 1) * E <= end;
     }
     // Columns outside the slice read as minus infinity: they take no part in the maximum or the sum.
-    __device__ __forceinline__ uint4 load(int j) const {
+    // `again`: they will be read once more, so L2 should keep them.
+    __device__ __forceinline__ uint4 load(int j, bool again = false) const {
         constexpr int E = DsType<T>::E;
-        if (j < nv && whole(j)) return __ldcs(reinterpret_cast<const uint4*>(base) + j);
+        if (j < nv && whole(j)) {
+            const uint4* at = reinterpret_cast<const uint4*>(base) + j;
+            return again ? __ldcg(at) : __ldcs(at);
+        }
         float f[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -241,7 +271,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
 
     uint4 x[kDsVecs];
 #pragma unroll
-    for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(tid + u * kDsThreads);
+    for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(tid + u * kDsThreads, MODE == kDsStep && sl.nv > kDsVecs * kDsThreads);
 
     // ---- the entries: columns, the teacher's values, the student's logits at them (wanted last, and fetched meanwhile)
     float early = 0.f;
@@ -292,13 +322,13 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
             top = warp_max(top);
             double sum = 0.0;
             for (int j = lane; j < p.k; j += 32)
-                if (s_idx[j] >= 0) sum += exp(s_lq[j] - top);
+                if (s_idx[j] >= 0) sum += exp_log(s_lq[j] - top);
             norm = top + log(warp_sum(sum));
         }
         double q_sum = 0.0;
         for (int j = lane; j < p.k; j += 32) {
             const double lq = s_lq[j] - norm;
-            const double q = s_idx[j] >= 0 && any ? exp(lq) : 0.0;
+            const double q = s_idx[j] >= 0 && any ? exp_log(lq) : 0.0;
             s_lq[j] = lq;
             s_q[j] = q;
             q_sum += q;
@@ -315,42 +345,48 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     const uint64_t c2 = pair2(p.c, p.c);
     if (MODE != kDsGrad) {
         float tm = -INFINITY, ts = 0.f;
+        // Half of the vectors at a time; where the row has more, theirs are asked for as soon as these are done with.
+        constexpr int HALF = kDsVecs / 2;
         for (int j0 = 0; j0 < sl.nv; j0 += kDsVecs * kDsThreads) {
-            if (j0 > 0) {
 #pragma unroll
-                for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(j0 + tid + u * kDsThreads);
-            }
-            const float cm = vec_max(x, kDsVecs, static_cast<const T*>(nullptr));
-            if (cm > tm) { ts *= tm == -INFINITY ? 0.f : ex2((tm - cm) * p.c); tm = cm; }
-            const float neg = tm == -INFINITY ? 0.f : -tm;
-            const uint64_t neg2 = pair2(neg, neg);
-            uint64_t acc = pair2(ts, 0.f);
+            for (int h = 0; h < 2; ++h) {
+                uint4* xh = x + HALF * h;
+                const float cm = vec_max<HALF>(xh, static_cast<const T*>(nullptr));
+                if (cm > tm) { ts *= tm == -INFINITY ? 0.f : ex2((tm - cm) * p.c); tm = cm; }
+                const float neg = tm == -INFINITY ? 0.f : -tm;
+                const uint64_t neg2 = pair2(neg, neg);
+                uint64_t acc = pair2(ts, 0.f);
 #pragma unroll
-            for (int u = 0; u < kDsVecs; ++u) {
-                forget(x[u]);
-                const int j = j0 + tid + u * kDsThreads;
-                if (j < sl.nv) {
-                    float f[E];
-                    DsType<T>::unpack(x[u], f);
-                    if (REST) {
-                        const uint32_t b = mark[j];
-                        if (b != 0) {
+                for (int u = 0; u < HALF; ++u) {
+                    forget(xh[u]);
+                    const int j = j0 + tid + (HALF * h + u) * kDsThreads;
+                    if (j < sl.nv) {
+                        float f[E];
+                        DsType<T>::unpack(xh[u], f);
+                        if (REST) {
+                            const uint32_t b = mark[j];
+                            if (b != 0) {
 #pragma unroll
-                            for (int e = 0; e < E; ++e)
-                                if (b >> e & 1u) f[e] = -INFINITY;
+                                for (int e = 0; e < E; ++e)
+                                    if (b >> e & 1u) f[e] = -INFINITY;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < E; e += 2) {
+                            float a, b;
+                            unpair2(mul2(add2(pair2(f[e], f[e + 1]), neg2), c2), a, b);
+                            acc = add2(acc, pair2(ex2(a), ex2(b)));
                         }
                     }
+                }
+                float a, b;
+                unpair2(acc, a, b);
+                ts = a + b;
+                if (j0 + kDsVecs * kDsThreads < sl.nv) {
 #pragma unroll
-                    for (int e = 0; e < E; e += 2) {
-                        float a, b;
-                        unpair2(mul2(add2(pair2(f[e], f[e + 1]), neg2), c2), a, b);
-                        acc = add2(acc, pair2(ex2(a), ex2(b)));
-                    }
+                    for (int u = 0; u < HALF; ++u) xh[u] = sl.load(j0 + tid + (kDsVecs + HALF * h + u) * kDsThreads, MODE == kDsStep);
                 }
             }
-            float a, b;
-            unpair2(acc, a, b);
-            ts = a + b;
         }
         // a warp's, then the slice's, then the row's
         float wm = tm;
@@ -402,15 +438,16 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     const RowTerms t = row_terms<REST>(m, static_cast<float>(R), z, static_cast<float>(q_sum), static_cast<float>(q_rest), static_cast<float>(mass));
     // loss, in 64 bits, by the warp that is given it (below, beside the gradient)
     auto write_loss = [&] {
-        const double ln2 = 0.69314718055994530942, cd = p.c, lz = log(static_cast<double>(t.Z));
+        const double ln2 = 0.69314718055994530942, cd = p.c;
+        const RowLogs lg = row_logs(t, q_rest, lane);
         double l = 0.0;
         for (int j = lane; j < p.k; j += 32) {
             const double q = s_q[j];
             if (s_idx[j] < 0 || q == 0.0) continue;
-            l += q * (s_lq[j] - (t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lz));
+            l += q * (s_lq[j] - (t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lg.z));
         }
         l = warp_sum(l);
-        if (REST && !(q_rest == 0.0)) l += q_rest * (log(q_rest) - log_rest(t, lz));
+        if (REST && !(q_rest == 0.0)) l += q_rest * (lg.q_rest - lg.p_rest);
         if (lane == 0) {
             p.loss[row] = any ? static_cast<float>(l) : 0.f;
             if (MODE == kDsLoss && p.saved != nullptr)
@@ -501,22 +538,16 @@ struct RowTeacher {          // what its entries come to
     float top, z;            // the student's largest logit of the set, its sum of 2^((s - top) c) over the set's columns
     int any, twice;          // something to learn from; a column in two entries
 };
-// Slots of the table in which a row's columns are looked for: a power of two, at least twice as many as there are entries.
-__host__ __device__ __forceinline__ int table_slots(int k) {
-    int n = 32;
-    while (n < 2 * k) n *= 2;
-    return n;
-}
-
+constexpr int kDsFilterBytes = 8192;     // a bit per column modulo 65536: has it been seen in this row?
 constexpr int kDsEntryBufs = 4;
 
 template <typename T>
 struct RowsSmem {            // byte offsets
-    int row, table, entries, entry_stride, mark, total;
+    int row, filter, entries, entry_stride, mark, total;
     __host__ __device__ RowsSmem(int slice, int k, int mark_bytes) {
         row = 0;
-        table = (slice / DsType<T>::E + 1) * 16;
-        entries = table + 2 * 4 * table_slots(k);      // one for each of the two warps
+        filter = (slice / DsType<T>::E + 1) * 16;
+        entries = filter + 2 * kDsFilterBytes;         // one for each of the two warps
         mark = entry_bytes(k);
         entry_stride = mark + (mark_bytes + 15) / 16 * 16;
         total = entries + kDsEntryBufs * entry_stride;
@@ -538,7 +569,7 @@ __device__ __forceinline__ float redux_max(float v) {
     return r;
 }
 
-template <typename T, bool REST>
+template <typename T, bool REST, int MODE>
 __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const DistillParams p) {
     constexpr int E = DsType<T>::E;
     extern __shared__ __align__(16) unsigned char ds_smem[];
@@ -573,6 +604,8 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
         for (int b = 0; b < 2; ++b) sb::init(slice_full(b), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    for (int i = tid; i < (lay.total - lay.filter) / 16; i += kDsRowsThreads)      // the filters and the marks are zero between rows
+        reinterpret_cast<uint4*>(ds_smem + lay.filter)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     if (ranks > 1) cluster_sync_all();                 // the others' barriers exist
     const T* logits = static_cast<const T*>(p.logits);
@@ -588,8 +621,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
         int2 f_idx[AHEAD];
         uint32_t f_val[AHEAD];
         float f_lse = 0.f, f_weight = 0.f;
-        const int slots = table_slots(p.k);
-        int* table = reinterpret_cast<int*>(ds_smem + lay.table) + turn * slots;
+        uint32_t* filter = reinterpret_cast<uint32_t*>(ds_smem + lay.filter + turn * kDsFilterBytes);
         auto raw_index = [&](size_t at) {
             if (p.index64) return static_cast<const int2*>(p.index)[at];
             return make_int2(static_cast<const int*>(p.index)[at], 0);
@@ -620,7 +652,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                 }
             }
             if (REST) f_lse = p.lse[row];
-            f_weight = p.dloss[row];
+            if (MODE == kDsStep) f_weight = p.dloss[row];
         };
         auto entries = [&](int row, int n) {           // of the n-th row of this CTA; its buffer is free, its first entries fetched
             const int b = n % kDsEntryBufs;
@@ -632,106 +664,122 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             uint8_t* s_first = reinterpret_cast<uint8_t*>(s_s + p.k);
             uint32_t* s_mark = reinterpret_cast<uint32_t*>(e0 + lay.mark);
             const T* r_logits = logits + static_cast<long long>(row) * p.ld;
-            const Slice<T> sl = slice_of(row);
+            const int shift = slice_of(row).shift - v0;
+            auto mark_word = [&](int i, int sh) { return s_mark + ((i + sh) / E >> 2); };
+            // the marks of the row that had this buffer go
+            if (REST && n >= kDsEntryBufs) {
+                const int old = slice_of(row - kDsEntryBufs * stride).shift - v0;
+#pragma unroll 2
+                for (int j = lane; j < p.k; j += 32) {
+                    const int i = s_idx[j];
+                    if (i >= v0 && i < v1) *mark_word(i, old) = 0u;
+                }
+                __syncwarp();
+            }
+            // the first 64 entries in registers, two of a lane side by side; the others after them
             T g[AHEAD];
-            int r_idx[AHEAD];
+            int idx[AHEAD];
+            double u_t[AHEAD];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                r_idx[u] = lane + 32 * u < p.k ? column(f_idx[u]) : -1;
-                if (r_idx[u] >= 0) g[u] = r_logits[r_idx[u]];
+                idx[u] = lane + 32 * u < p.k ? column(f_idx[u]) : -1;
+                if (idx[u] >= 0) g[u] = r_logits[idx[u]];
             }
-            for (int j = lane; j < slots / 4; j += 32) reinterpret_cast<int4*>(table)[j] = make_int4(-1, -1, -1, -1);
-            if (REST)
-                for (int j = lane; j < (p.mark_bytes + 15) / 16; j += 32) reinterpret_cast<uint4*>(s_mark)[j] = make_uint4(0, 0, 0, 0);
-            if (lane < 4) s_idx[p.k + lane] = -1;
-            __syncwarp();
-            double top = -INFINITY;
-            int any = 0, finite = 0, twice = 0, columns = 0;
-            auto take = [&](int j, int i, float value) {
-                const double u = static_cast<double>(value) * p.inv_t;
+            int seen = 0, columns = 0;
+            auto enter = [&](int j, int i) {
                 s_idx[j] = i;
-                s_lq[j] = u;
                 s_first[j] = i >= 0;
                 if (i >= 0) {
-                    any = 1;
                     ++columns;
-                    if (!REST) { top = fmax(top, u); finite |= !(u == -INFINITY); }
-                    // is the column there already?  A table with open slots; entries that lose a slot to another look at the next
-                    int at = static_cast<int>(static_cast<uint32_t>(i) * 2654435769u >> 8) & (slots - 1);
-                    for (;;) {
-                        const int was = atomicCAS(table + at, -1, i);
-                        if (was == -1) break;
-                        if (was == i) { twice = 1; break; }
-                        at = (at + 1) & (slots - 1);
-                    }
-                    if (REST && i >= v0 && i < v1) {
-                        const int e = i - v0 + sl.shift;
-                        atomicOr(s_mark + (e / E >> 2), 1u << ((e / E & 3) * 8 + e % E));
-                    }
+                    seen |= atomicOr(filter + (i >> 5 & (kDsFilterBytes / 4 - 1)), 1u << (i & 31)) >> (i & 31) & 1u;
+                    if (REST && i >= v0 && i < v1) atomicOr(mark_word(i, shift), 1u << (((i + shift) / E & 3) * 8 + (i + shift) % E));
                 }
             };
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                if (32 * u >= p.k) break;
-                const int j = lane + 32 * u;
-                if (j < p.k) take(j, r_idx[u], teacher_logit(f_val[u]));
+                if (lane + 32 * u < p.k) enter(lane + 32 * u, idx[u]);
+                u_t[u] = idx[u] >= 0 ? static_cast<double>(teacher_logit(f_val[u])) * p.inv_t : -INFINITY;
             }
             const float lse = f_lse, weight = f_weight;
             fetch(row + 2 * stride);
+            double top = fmax(u_t[0], u_t[1]);
+            bool bad = u_t[0] != u_t[0] || u_t[1] != u_t[1];
 #pragma unroll 1
             for (int j = lane + 32 * AHEAD; j < p.k; j += 32) {
                 const size_t at = static_cast<size_t>(row) * p.k + j;
                 const int i = column(raw_index(at));
-                take(j, i, teacher_logit(raw_value(at)));
+                const double u = i >= 0 ? static_cast<double>(teacher_logit(raw_value(at))) * p.inv_t : -INFINITY;
+                enter(j, i);
                 s_s[j] = i >= 0 ? DsType<T>::one(r_logits[i]) : 0.f;
+                s_lq[j] = u;
+                top = fmax(top, u);
+                bad = bad || u != u;
             }
             __syncwarp();
-            any = __any_sync(0xffffffffu, any);
-            if (__any_sync(0xffffffffu, twice)) {      // which entry is its column's first: the one with the lowest number
-                twice = 1;
-                columns = 0;
+            columns = static_cast<int>(__reduce_add_sync(0xffffffffu, columns));
+            int any = columns, twice = 0;
+            if (__any_sync(0xffffffffu, seen)) {       // perhaps a column twice (certainly so up to 65536 columns): which entry is its column's first
                 for (int j = lane; j < p.k; j += 32) {
                     const int i = s_idx[j];
-                    bool again = i < 0;
+                    bool again = false;
                     for (int o = 0; o < j; ++o) again = again || s_idx[o] == i;
-                    s_first[j] = !again;
-                    columns += !again;
+                    s_first[j] = i >= 0 && !again;
+                    twice += i >= 0 && again;
                 }
+                twice = static_cast<int>(__reduce_add_sync(0xffffffffu, twice));
+                columns -= twice;
             }
-            double norm;
-            if (REST) norm = lse;
-            else {
-                any = __any_sync(0xffffffffu, finite);
+#pragma unroll 2
+            for (int j = lane; j < p.k; j += 32) {     // the filter is zero again
+                const int i = s_idx[j];
+                if (i >= 0) filter[i >> 5 & (kDsFilterBytes / 4 - 1)] = 0u;
+            }
+            // the teacher's probabilities
+            double norm = lse;
+            if (!REST) {
+                any = __any_sync(0xffffffffu, top > -INFINITY || bad);       // not all of them minus infinity
                 top = warp_max(top);
-                double sum = 0.0;
+                if (top == -INFINITY) top = 0.0;
+                double sum = exp_log(u_t[0] - top) + exp_log(u_t[1] - top);
 #pragma unroll 1
-                for (int j = lane; j < p.k; j += 32)
-                    if (s_idx[j] >= 0) sum += exp(s_lq[j] - top);
+                for (int j = lane + 32 * AHEAD; j < p.k; j += 32) sum += exp_log(s_lq[j] - top);
                 norm = top + log(warp_sum(sum));
             }
             double q_sum = 0.0;
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int j = lane + 32 * u;
+                const double lq = u_t[u] - norm, q = idx[u] >= 0 && any ? exp_log(lq) : 0.0;
+                if (j < p.k) { s_lq[j] = lq; s_q[j] = q; }
+                q_sum += q;
+            }
 #pragma unroll 1
-            for (int j = lane; j < p.k; j += 32) {
-                const double lq = s_lq[j] - norm;
-                const double q = s_idx[j] >= 0 && any ? exp(lq) : 0.0;
+            for (int j = lane + 32 * AHEAD; j < p.k; j += 32) {
+                const double lq = s_lq[j] - norm, q = s_idx[j] >= 0 && any ? exp_log(lq) : 0.0;
                 s_lq[j] = lq;
                 s_q[j] = q;
                 q_sum += q;
             }
             q_sum = warp_sum(q_sum);
-            columns = static_cast<int>(__reduce_add_sync(0xffffffffu, columns));
+            // the student's logits
+            float sv[AHEAD], s_top = -INFINITY, z = 0.f;
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                if (lane + 32 * u < p.k) s_s[lane + 32 * u] = r_idx[u] >= 0 ? DsType<T>::one(g[u]) : 0.f;
-            float s_top = -INFINITY, z = 0.f;
+            for (int u = 0; u < AHEAD; ++u) {
+                sv[u] = idx[u] >= 0 ? DsType<T>::one(g[u]) : -INFINITY;
+                if (lane + 32 * u < p.k) s_s[lane + 32 * u] = sv[u];
+            }
             if (REST) {
+                s_top = fmaxf(sv[0], sv[1]);
 #pragma unroll 1
-                for (int j = lane; j < p.k; j += 32)
+                for (int j = lane + 32 * AHEAD; j < p.k; j += 32)
                     if (s_idx[j] >= 0) s_top = fmaxf(s_top, s_s[j]);
                 s_top = redux_max(s_top);
                 const float r = s_top == -INFINITY ? 0.f : s_top;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u)
+                    if (idx[u] >= 0 && (twice == 0 || s_first[lane + 32 * u])) z += ex2((sv[u] - r) * p.c);
 #pragma unroll 1
-                for (int j = lane; j < p.k; j += 32)
+                for (int j = lane + 32 * AHEAD; j < p.k; j += 32)
                     if (s_first[j]) z += ex2((s_s[j] - r) * p.c);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
@@ -794,17 +842,20 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                 const double* s_lq = s_q + p.k;
                 const int* s_idx = reinterpret_cast<const int*>(s_lq + p.k);
                 const float* s_s = reinterpret_cast<const float*>(s_idx + p.k + 4);
-                const double lz = log(static_cast<double>(t.Z));
+                const RowLogs lg = row_logs(t, te.q_rest, lane);
                 double l = 0.0;
 #pragma unroll 1
                 for (int j = lane; j < p.k; j += 32) {
                     const double q = s_q[j];
                     if (s_idx[j] < 0 || q == 0.0) continue;
-                    l += q * (s_lq[j] - (t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lz));
+                    l += q * (s_lq[j] - (t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lg.z));
                 }
                 l = warp_sum(l);
-                if (REST && !(te.q_rest == 0.0)) l += te.q_rest * (log(te.q_rest) - log_rest(t, lz));
-                if (lane == 0) p.loss[row] = te.any ? static_cast<float>(l) : 0.f;
+                if (REST && !(te.q_rest == 0.0)) l += te.q_rest * (lg.q_rest - lg.p_rest);
+                if (lane == 0) {
+                    p.loss[row] = te.any ? static_cast<float>(l) : 0.f;
+                    if (MODE == kDsLoss && p.saved != nullptr) *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) = make_float4(t.ref, t.Z, t.R, 0.f);
+                }
             }
             __syncwarp();
         }
@@ -844,7 +895,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             if (lane == 0) sb::arrive(row_empty);
 
             // ---- maximum and sum of exponentials (outside the set with REST) of a warp, the slice, the row
-            const float tm = redux_max(vec_max(x, kDsVecs, static_cast<const T*>(nullptr)));
+            const float tm = redux_max(vec_max<kDsVecs>(x, static_cast<const T*>(nullptr)));
             float ws;
             {
                 const float neg = tm == -INFINITY ? 0.f : -tm;
@@ -910,33 +961,35 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             const float factor = any ? t.factor * static_cast<float>(te.d) : 0.f;
 
             // ---- the gradient: one factor for the whole row, then the listed columns
-            T* r_grad = static_cast<T*>(p.grad) + static_cast<long long>(row) * p.ldg;
-            T* g_base = r_grad + v0 - sl.shift;
-            const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
-            const uint64_t neg2 = pair2(-t.ref, -t.ref), factor2 = pair2(factor, factor);
+            T* r_grad = MODE == kDsStep ? static_cast<T*>(p.grad) + static_cast<long long>(row) * p.ldg : nullptr;
+            if (MODE == kDsStep) {
+                T* g_base = r_grad + v0 - sl.shift;
+                const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
+                const uint64_t neg2 = pair2(-t.ref, -t.ref), factor2 = pair2(factor, factor);
 #pragma unroll
-            for (int u = 0; u < kDsVecs; ++u) {
-                forget(x[u]);
-                const int j = tid + u * kDsThreads;
-                if (j < sl.nv) {
-                    float f[E];
-                    DsType<T>::unpack(x[u], f);
+                for (int u = 0; u < kDsVecs; ++u) {
+                    forget(x[u]);
+                    const int j = tid + u * kDsThreads;
+                    if (j < sl.nv) {
+                        float f[E];
+                        DsType<T>::unpack(x[u], f);
 #pragma unroll
-                    for (int e = 0; e < E; e += 2) {
-                        float v, w;
-                        unpair2(mul2(add2(pair2(f[e], f[e + 1]), neg2), c2), v, w);
-                        unpair2(mul2(pair2(ex2(v), ex2(w)), factor2), f[e], f[e + 1]);
-                    }
-                    if (!any) {
+                        for (int e = 0; e < E; e += 2) {
+                            float v, w;
+                            unpair2(mul2(add2(pair2(f[e], f[e + 1]), neg2), c2), v, w);
+                            unpair2(mul2(pair2(ex2(v), ex2(w)), factor2), f[e], f[e + 1]);
+                        }
+                        if (!any) {
 #pragma unroll
-                        for (int e = 0; e < E; ++e) f[e] = 0.f;
-                    }
-                    if (vectors && sl.whole(j)) __stcs(reinterpret_cast<uint4*>(g_base) + j, DsType<T>::pack(f));
-                    else {
+                            for (int e = 0; e < E; ++e) f[e] = 0.f;
+                        }
+                        if (vectors && sl.whole(j)) __stcs(reinterpret_cast<uint4*>(g_base) + j, DsType<T>::pack(f));
+                        else {
 #pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const int i = j * E + e;
-                            if (i >= sl.shift && i < sl.end) g_base[i] = DsType<T>::round(f[e]);
+                            for (int e = 0; e < E; ++e) {
+                                const int i = j * E + e;
+                                if (i >= sl.shift && i < sl.end) g_base[i] = DsType<T>::round(f[e]);
+                            }
                         }
                     }
                 }
@@ -944,7 +997,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             uint32_t gave_up;                          // the listed columns are written over; and who has given up says so
             asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
                          : "=r"(gave_up) : "r"(ok ? 0u : 1u), "n"(kDsThreads) : "memory");
-            if (any) {
+            if (MODE == kDsStep && any) {
                 for (int j = tid; j < p.k; j += kDsThreads) {
                     const int i = s_idx[j];
                     if (!s_first[j] || i < v0 || i >= v1) continue;
@@ -994,13 +1047,13 @@ static cudaError_t distill_launch_as(const DistillParams& p, int cluster, size_t
     return cudaLaunchKernelEx(&cfg, distill_kernel<T, REST, MODE>, p);
 }
 // Clusters of the many-rows kernel that are resident at once.
-template <typename T, bool REST>
+template <typename T, bool REST, int MODE>
 static int rows_resident(int cluster, size_t smem) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
     static std::atomic<bool> attr_set[64];    // zero-initialised; set-up is idempotent, so a race repeats it harmlessly
     if (dev < 0 || dev >= 64 || !attr_set[dev]) {
-        if (cudaFuncSetAttribute(distill_rows_kernel<T, REST>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024) != cudaSuccess) {
+        if (cudaFuncSetAttribute(distill_rows_kernel<T, REST, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024) != cudaSuccess) {
             (void)cudaGetLastError();
             return 0;
         }
@@ -1008,7 +1061,7 @@ static int rows_resident(int cluster, size_t smem) {
     }
     return smem <= 110 * 1024 ? 2 * device_sm_count() / cluster : 0;
 }
-template <typename T, bool REST>
+template <typename T, bool REST, int MODE>
 static cudaError_t rows_launch(const DistillParams& p, int cluster, int clusters, size_t smem, cudaStream_t s) {
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
@@ -1021,27 +1074,28 @@ static cudaError_t rows_launch(const DistillParams& p, int cluster, int clusters
     attr.val.clusterDim.x = static_cast<unsigned>(cluster); attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, distill_rows_kernel<T, REST>, p);
+    return cudaLaunchKernelEx(&cfg, distill_rows_kernel<T, REST, MODE>, p);
 }
 // The many-rows kernel, where a row fits a cluster's registers and there are more rows than clusters at once (1 if not taken).
-template <typename T, bool REST>
+template <typename T, bool REST, int MODE>
 static int rows_try_as(const DistillParams& p, int cluster, cudaStream_t s) {
     if (p.slice / DsType<T>::E + 1 > kDsThreads * kDsVecs) return 1;
     const RowsSmem<T> lay(p.slice, p.k, p.mark_bytes);
-    const int clusters = rows_resident<T, REST>(cluster, static_cast<size_t>(lay.total));
+    const int clusters = rows_resident<T, REST, MODE>(cluster, static_cast<size_t>(lay.total));
     if (clusters < 1 || p.M <= clusters) return 1;
-    SLIM_CUDA_TRY((rows_launch<T, REST>(p, cluster, clusters, static_cast<size_t>(lay.total), s)));
+    SLIM_CUDA_TRY((rows_launch<T, REST, MODE>(p, cluster, clusters, static_cast<size_t>(lay.total), s)));
     return SLIM_OK;
 }
-template <typename T>
+template <typename T, int MODE>
 static int rows_try_rest(const DistillParams& p, int cluster, cudaStream_t s) {
-    return p.lse != nullptr ? rows_try_as<T, true>(p, cluster, s) : rows_try_as<T, false>(p, cluster, s);
+    return p.lse != nullptr ? rows_try_as<T, true, MODE>(p, cluster, s) : rows_try_as<T, false, MODE>(p, cluster, s);
 }
+template <int MODE>
 static int rows_try(const DistillParams& p, int type, int cluster, cudaStream_t s) {
     switch (type) {
-        case SLIM_F32: return rows_try_rest<float>(p, cluster, s);
-        case SLIM_F16: return rows_try_rest<__half>(p, cluster, s);
-        default: return rows_try_rest<__nv_bfloat16>(p, cluster, s);
+        case SLIM_F32: return rows_try_rest<float, MODE>(p, cluster, s);
+        case SLIM_F16: return rows_try_rest<__half, MODE>(p, cluster, s);
+        default: return rows_try_rest<__nv_bfloat16, MODE>(p, cluster, s);
     }
 }
 
@@ -1077,12 +1131,6 @@ static int distill(int mode, const void* logits, int type, long long ld, const v
         !aligned_to(lse, 4) || !aligned_to(dloss, 4) || !aligned_to(loss, 4) || !aligned16(saved))
         return SLIM_ERR_ALIGNMENT;
     const int E = 16 / es, held = kDsThreads * kDsVecs;            // vectors that a CTA's registers hold
-    // A cluster as large as the one pass needs to hold a row, or as fills the SMs twice while a thread still has a vector.
-    const int vecs = V / E + 2;
-    int cluster = 1;
-    while (cluster < kDsMaxCluster && ((mode == kDsStep && vecs > cluster * (held - 1)) || vecs > cluster * 65536 / 2 ||
-                                       (static_cast<long long>(M) * cluster < 2 * device_sm_count() && vecs > cluster * kDsThreads)))
-        cluster *= 2;
     DistillParams p;
     memset(&p, 0, sizeof p);
     p.logits = logits; p.index = index; p.value = value; p.lse = lse; p.dloss = dloss; p.loss = loss; p.saved = saved; p.grad = grad;
@@ -1092,15 +1140,31 @@ static int distill(int mode, const void* logits, int type, long long ld, const v
     p.M = M; p.V = V; p.k = k;
     p.index64 = index_bytes == 8;
     p.value_type = value_type;
-    p.ranks = cluster;
-    p.slice = ((V + cluster - 1) / cluster + E - 1) / E * E;
-    p.mark_bytes = lse != nullptr ? (p.slice / E + 1 + 3) / 4 * 4 : 0;
-    const size_t smem = static_cast<size_t>(entry_bytes(k)) + p.mark_bytes;
+    auto cut = [&](int cluster) {
+        p.ranks = cluster;
+        p.slice = ((V + cluster - 1) / cluster + E - 1) / E * E;
+        p.mark_bytes = lse != nullptr ? (p.slice / E + 1 + 3) / 4 * 4 : 0;
+    };
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (mode == kDsStep) {
-        const int taken = rows_try(p, type, cluster, s);
+    const int vecs = V / E + 2;
+    // Many rows that one CTA's registers hold, or for the step two CTAs': the kernel that takes row after row.  (us, that one / a CTA per
+    // row: step of 4096 x 32000 bf16 127 / 173, of 2000 x 40000 by two 99 / 122; loss of 4096 x 32000 71 / 106, of 4096 x 8000 49 / 91.  By three and more the CTAs of
+    // a row wait for each other longer than the second reading, from L2, takes: 1024 x 65536 125 / 78, 512 x 152064 121 / 93, 777 x 50257 fp32 106 / 84.)
+    if (mode != kDsGrad && vecs <= (mode == kDsStep ? 2 : 1) * (held - 1)) {
+        cut(vecs <= held - 1 ? 1 : 2);
+        const int taken = mode == kDsStep ? rows_try<kDsStep>(p, type, p.ranks, s) : rows_try<kDsLoss>(p, type, p.ranks, s);
         if (taken <= 0) return taken;
     }
+    // Otherwise the cluster that ends soonest: a CTA has its part of a row to read, and what a row costs besides takes as long as some 6500 vectors.
+    int cluster = 1;
+    double least = 1e30;
+    for (int c = 1; c <= kDsMaxCluster; ++c) {
+        const long long waves = (static_cast<long long>(M) * c + 2 * device_sm_count() - 1) / (2 * device_sm_count());
+        const double t = static_cast<double>(waves) * (static_cast<double>(vecs) / c + 6500.0);
+        if (vecs <= c * 32768 && t < 0.98 * least) { least = t; cluster = c; }
+    }
+    cut(cluster);
+    const size_t smem = static_cast<size_t>(entry_bytes(k)) + p.mark_bytes;
     SLIM_CUDA_TRY(mode == kDsLoss ? distill_launch<kDsLoss>(p, type, cluster, smem, s)
                   : mode == kDsGrad ? distill_launch<kDsGrad>(p, type, cluster, smem, s) : distill_launch<kDsStep>(p, type, cluster, smem, s));
     return SLIM_OK;
