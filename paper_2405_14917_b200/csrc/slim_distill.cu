@@ -268,6 +268,8 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     const int v0 = min(p.V, rank * p.slice), v1 = min(p.V, v0 + p.slice);
     const T* r_logits = static_cast<const T*>(p.logits) + static_cast<long long>(row) * p.ld;
     const Slice<T> sl(r_logits + v0, v1 - v0);
+    pdl_launch_dependents();
+    pdl_wait();
 
     uint4 x[kDsVecs];
 #pragma unroll
@@ -608,6 +610,8 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
         reinterpret_cast<uint4*>(ds_smem + lay.filter)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     if (ranks > 1) cluster_sync_all();                 // the others' barriers exist
+    pdl_launch_dependents();
+    pdl_wait();
     const T* logits = static_cast<const T*>(p.logits);
     auto slice_of = [&](int row) { return Slice<T>(logits + static_cast<long long>(row) * p.ld + v0, v1 - v0); };
     const double ln2 = 0.69314718055994530942, cd = p.c;
@@ -1039,11 +1043,13 @@ static cudaError_t distill_launch_as(const DistillParams& p, int cluster, size_t
     cfg.blockDim = dim3(kDsThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = static_cast<unsigned>(cluster); attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // set up beside the kernel ahead, which it waits for
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, distill_kernel<T, REST, MODE>, p);
 }
 // Clusters of the many-rows kernel that are resident at once.
@@ -1069,11 +1075,13 @@ static cudaError_t rows_launch(const DistillParams& p, int cluster, int clusters
     cfg.blockDim = dim3(kDsRowsThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = static_cast<unsigned>(cluster); attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster); attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;       // set up beside the kernel ahead, which it waits for
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, distill_rows_kernel<T, REST, MODE>, p);
 }
 // The many-rows kernel, where a row fits a cluster's registers and there are more rows than clusters at once (1 if not taken).
