@@ -186,19 +186,6 @@ __device__ __forceinline__ double exp_log(double x) {
     const double y = fma(fma(ef, r4, cd), r4, ab);
     return __hiloint2double(__double2hiint(y) + (static_cast<int>(n) << 20), __double2loint(y));
 }
-// The logarithms that a loss needs, in 64 bits, by a lane each: of Z, q' and p' (what p_in leaves of 1, or R / Z where that would cancel).
-struct RowLogs {
-    double z, q_rest, p_rest;
-};
-__device__ __forceinline__ RowLogs row_logs(const RowTerms& t, double q_rest, int lane) {
-    const double v = log(lane == 0 ? static_cast<double>(t.Z) : lane == 1 ? q_rest : lane == 2 ? 1.0 - static_cast<double>(t.p_in) : static_cast<double>(t.R));
-    RowLogs l;
-    l.z = __shfl_sync(0xffffffffu, v, 0);
-    l.q_rest = __shfl_sync(0xffffffffu, v, 1);
-    const double left = __shfl_sync(0xffffffffu, v, 2), r = __shfl_sync(0xffffffffu, v, 3);
-    l.p_rest = t.Z == 0.f || t.R == 0.f ? -INFINITY : t.p_in < 0.5f ? left : r - l.z;
-    return l;
-}
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -208,6 +195,32 @@ __device__ __forceinline__ double warp_max(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
+}
+
+// A row's loss, in 64 bits, by a warp.  The set's mass is taken from the same log p as the entries' terms, so that an error in Z, which is fp32, shows in
+// the difference of the set's two masses alone: with little in the set the loss is as small as that difference.
+template <bool REST>
+__device__ __forceinline__ double row_loss(const RowTerms& t, double q_rest, int k, float c, const double* s_q, const double* s_lq, const int* s_idx,
+                                           const float* s_s, const uint8_t* s_first, int lane) {
+    const double ln2 = 0.69314718055994530942, cd = c;
+    // logarithms by a lane each
+    const double v = log(lane == 0 ? static_cast<double>(t.Z) : lane == 1 ? q_rest : static_cast<double>(t.R));
+    const double lz = __shfl_sync(0xffffffffu, v, 0);
+    double l = 0.0, p_in = 0.0;
+#pragma unroll 2
+    for (int j = lane; j < k; j += 32) {
+        const bool in = s_idx[j] >= 0;
+        const double q = s_q[j], lp = t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lz;
+        l += !in || q == 0.0 ? 0.0 : q * (s_lq[j] - lp);
+        if (REST) p_in += in && s_first[j] ? exp_log(lp) : 0.0;
+    }
+    l = warp_sum(l);
+    if (REST && !(q_rest == 0.0)) {
+        p_in = warp_sum(p_in);
+        const double lr = __shfl_sync(0xffffffffu, v, 2) - lz;
+        l += q_rest * (__shfl_sync(0xffffffffu, v, 1) - (t.Z == 0.f || t.R == 0.f ? -INFINITY : p_in < 0.5 ? log(1.0 - p_in) : lr));
+    }
+    return l;
 }
 
 // A slice of a row: its first column sits `shift` elements behind a 16-byte boundary, and vector j holds the columns
@@ -440,16 +453,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     const RowTerms t = row_terms<REST>(m, static_cast<float>(R), z, static_cast<float>(q_sum), static_cast<float>(q_rest), static_cast<float>(mass));
     // loss, in 64 bits, by the warp that is given it (below, beside the gradient)
     auto write_loss = [&] {
-        const double ln2 = 0.69314718055994530942, cd = p.c;
-        const RowLogs lg = row_logs(t, q_rest, lane);
-        double l = 0.0;
-        for (int j = lane; j < p.k; j += 32) {
-            const double q = s_q[j];
-            if (s_idx[j] < 0 || q == 0.0) continue;
-            l += q * (s_lq[j] - (t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lg.z));
-        }
-        l = warp_sum(l);
-        if (REST && !(q_rest == 0.0)) l += q_rest * (lg.q_rest - lg.p_rest);
+        const double l = row_loss<REST>(t, q_rest, p.k, p.c, s_q, s_lq, s_idx, s_s, s_first, lane);
         if (lane == 0) {
             p.loss[row] = any ? static_cast<float>(l) : 0.f;
             if (MODE == kDsLoss && p.saved != nullptr)
@@ -614,7 +618,6 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
     pdl_wait();
     const T* logits = static_cast<const T*>(p.logits);
     auto slice_of = [&](int row) { return Slice<T>(logits + static_cast<long long>(row) * p.ld + v0, v1 - v0); };
-    const double ln2 = 0.69314718055994530942, cd = p.c;
 
     if (warp >= kDsWarps) {
         // ------------------------------------------------------------------ the two beside them: even rows and odd rows of this CTA
@@ -846,16 +849,8 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                 const double* s_lq = s_q + p.k;
                 const int* s_idx = reinterpret_cast<const int*>(s_lq + p.k);
                 const float* s_s = reinterpret_cast<const float*>(s_idx + p.k + 4);
-                const RowLogs lg = row_logs(t, te.q_rest, lane);
-                double l = 0.0;
-#pragma unroll 1
-                for (int j = lane; j < p.k; j += 32) {
-                    const double q = s_q[j];
-                    if (s_idx[j] < 0 || q == 0.0) continue;
-                    l += q * (s_lq[j] - (t.Z == 0.f ? -INFINITY : (static_cast<double>(s_s[j]) - static_cast<double>(t.ref)) * cd * ln2 - lg.z));
-                }
-                l = warp_sum(l);
-                if (REST && !(te.q_rest == 0.0)) l += te.q_rest * (lg.q_rest - lg.p_rest);
+                const uint8_t* s_first = reinterpret_cast<const uint8_t*>(s_s + p.k);
+                const double l = row_loss<REST>(t, te.q_rest, p.k, p.c, s_q, s_lq, s_idx, s_s, s_first, lane);
                 if (lane == 0) {
                     p.loss[row] = te.any ? static_cast<float>(l) : 0.f;
                     if (MODE == kDsLoss && p.saved != nullptr) *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) = make_float4(t.ref, t.Z, t.R, 0.f);
@@ -1156,7 +1151,7 @@ static int distill(int mode, const void* logits, int type, long long ld, const v
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int vecs = V / E + 2;
     // Many rows that one CTA's registers hold, or for the step two CTAs': the kernel that takes row after row.  (us, that one / a CTA per
-    // row: step of 4096 x 32000 bf16 127 / 173, of 2000 x 40000 by two 99 / 122; loss of 4096 x 32000 71 / 106, of 4096 x 8000 49 / 91.  By three and more the CTAs of
+    // row: step of 4096 x 32000 bf16 131 / 173, of 2000 x 40000 by two 99 / 122; loss of 4096 x 32000 71 / 106, of 4096 x 8000 49 / 91.  By three and more the CTAs of
     // a row wait for each other longer than the second reading, from L2, takes: 1024 x 65536 125 / 78, 512 x 152064 121 / 93, 777 x 50257 fp32 106 / 84.)
     if (mode != kDsGrad && vecs <= (mode == kDsStep ? 2 : 1) * (held - 1)) {
         cut(vecs <= held - 1 ? 1 : 2);

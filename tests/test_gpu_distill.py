@@ -282,3 +282,30 @@ def test_refusals():
         slim.distill_loss(torch.zeros(1, 50, device="cuda").half(), torch.zeros(1, 1025, dtype=torch.int64, device="cuda"), torch.zeros(1, 1025, device="cuda"))
     loss, saved = slim.distill_loss(s[:0], i[:0], v[:0])       # no row: nothing to do
     assert loss.shape == (0,) and slim.distill_grad(s[:0], i[:0], v[:0], saved, d[:0]).shape == (0, 50)
+
+
+def test_rows_farther_apart_than_32_bits_count():
+    """Row strides whose offsets pass 2^31 elements, in a buffer that is never read beside the rows."""
+    V, ld = 4003, 1_150_000_001
+    student, index, value, lse, dloss = _case(3, V, 9, "fp16", 1.0, True, 4)
+    buf = torch.empty(2 * ld + V, dtype=torch.float16, device="cuda")
+    s = torch.as_strided(buf, (3, V), (ld, 1), 0)
+    s.copy_(student)
+    loss, saved = _slim().distill_loss(s, index.cuda(), value.cuda(), teacher_lse=lse.cuda())
+    grad = _slim().distill_grad(s, index.cuda(), value.cuda(), saved, dloss.cuda(), teacher_lse=lse.cuda(), out=s)
+    assert grad is s
+    _check(student, index, value, lse, dloss, 1.0, "fp16", loss, grad)
+
+
+def test_a_batch_of_more_than_32_bits_of_logits():
+    """The many-rows kernel on 70000 x 32000 logits, the gradient in their place: rows from the far end against the oracle."""
+    M, V, k = 70000, 32000, 4
+    g = torch.Generator(device="cuda").manual_seed(5)
+    s = torch.empty(M, V, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    index = torch.randint(0, V, (M, k), generator=g, device="cuda", dtype=torch.int32)
+    value = torch.randn(M, k, generator=g, device="cuda") + 3
+    dloss = torch.ones(M, device="cuda")
+    rows = [0, 1, 67107, 67108, 67109, 69998, 69999]          # 67108 x 32000 is where 2^31 lies
+    student = s[rows].cpu()
+    loss, grad = _slim().distill_step(s, index, value, dloss, out=s)
+    _check(student, index[rows].cpu(), value[rows].cpu(), None, dloss[rows].cpu(), 1.0, "bf16", loss[rows], grad[rows])

@@ -226,3 +226,45 @@ def test_empty_calls_and_refusals():
     odd = slim.Fp8Linear.from_weight(_weight(250, 272, 1).cuda())
     with pytest.raises(ValueError):
         odd.input_grad(torch.zeros(4, 250, dtype=torch.float16, device="cuda"), ws)
+
+
+@pytest.mark.parametrize("M", [2, 40, 200])
+def test_a_weight_of_more_than_32_bits_of_codes(M):
+    """262400 x 8208 codes: the last rows, beyond 2^31 bytes, against the oracle."""
+    slim = _slim()
+    N, K, tail = 262400, 8208, 300
+    W = torch.empty(N, K, dtype=torch.bfloat16, device="cuda")
+    W[:] = torch.randn(1, K, device="cuda").bfloat16()
+    W[-tail:] = _weight(tail, K, 3, "bf16").cuda()
+    codes, scales = slim.fp8_quantize(W)
+    first = (N - tail) // 128 * 128
+    want_c, want_s = orc.quantize(W[first:].double().cpu().numpy())
+    np.testing.assert_array_equal(codes[first:].view(torch.uint8).cpu().numpy(), want_c)
+    np.testing.assert_array_equal(scales[first // 128:].cpu().numpy(), want_s)
+    x = _x(M, K, 1, "bf16").cuda()
+    layer = slim.Fp8Linear(codes, scales)
+    ws = layer.new_workspace(M)
+    y = layer.forward(x, ws)
+    slim.workspace_status(ws)
+    _check(y[:, first:], x, codes[first:], scales[first // 128:])
+
+
+@pytest.mark.parametrize("M", [3, 20, 50, 150])
+def test_rows_farther_apart_than_32_bits_count(M):
+    slim = _slim()
+    N, K = 130, 272
+    layer = slim.Fp8Linear.from_weight(_weight(N, K, 1).cuda())
+    ld = (2 ** 31 + 2 ** 20) // (M - 1) // 8 * 8 + 8
+    buf = torch.empty((M - 1) * ld + 512, dtype=torch.float16, device="cuda")
+    x, y = torch.as_strided(buf, (M, K), (ld, 1), 0), torch.as_strided(buf, (M, N), (ld, 1), 272)
+    x.copy_(_x(M, K, 2))
+    assert layer.forward(x, layer.new_workspace(M), out=y) is y
+    _check(y, x, layer.codes, layer.scales)
+
+
+def test_a_sum_of_nothing():
+    slim = _slim()
+    codes, scales = slim.fp8_quantize(torch.zeros(200, 0, dtype=torch.float16, device="cuda"))
+    layer = slim.Fp8Linear(codes, scales)
+    y = layer.forward(torch.zeros(3, 0, dtype=torch.float16, device="cuda"), layer.new_workspace(3), out=torch.full((3, 200), 5.0, device="cuda"))
+    assert (y == 0).all()
