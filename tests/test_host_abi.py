@@ -238,7 +238,7 @@ def test_8_bit_layer_argument_errors_and_sizes(slim):
     a = 1 << 20
     out = ctypes.c_size_t(0)
     assert L.slim_fp8_workspace_bytes(1, 4096, 4096, ctypes.byref(out)) == 0 and out.value == 1280        # header and flags
-    assert L.slim_fp8_workspace_bytes(100, 4096, 400, ctypes.byref(out)) == 0 and out.value >= 1280 + 100 * 400 + 4 * 4 * 100
+    assert L.slim_fp8_workspace_bytes(100, 4096, 400, ctypes.byref(out)) == 0 and out.value >= 1280 + 100 * 400 + 4 * 100        # codes, and a word of four exponents per token
     assert L.slim_fp8_workspace_bytes(100, 4096, 400, None) == -1
     assert L.slim_fp8_workspace_bytes(-1, 16, 16, ctypes.byref(out)) == -1
     assert L.slim_fp8_workspace_bytes(1, 16, 24, ctypes.byref(out)) == -2                                 # K not a multiple of 16
