@@ -9,11 +9,13 @@
 // sum_j q_j + q' for the listed columns, that less q' / p' for all others.  So a row needs its maximum, its sum of exponentials
 // outside the listed columns, and k logits; then its gradient is one multiplication per element and k corrections.
 //
-// Bound: HBM (a row is read once, its gradient written once).  A row belongs to a cluster of 1 to 8 CTAs of 512 threads, each with
-// a slice of its columns; a thread takes eight 16-byte vectors of it at a time and, in the one-pass form, keeps them in registers
-// between the statistics and the gradient, so that the logits are not read again.  The slice statistics
-// meet through distributed shared memory; every sum has a fixed order.  Sums over the vocabulary are fp32 per thread (64 terms at a time) and fp64 from
-// there on; what is computed per row and per entry is fp64, because a small loss is the difference of large terms.
+// Bound: HBM (a row is read once, its gradient written once), with two ex2 per element next to it.  Two kernels: a CTA or cluster per row, and
+// one that takes row after row (below).  A row belongs to 1 to 8 CTAs of 512 threads, each with a slice of its columns; a thread takes eight 16-byte
+// vectors of it at a time and, in the one call for both, keeps them in registers between the statistics and the gradient; a longer row is read a second
+// time, from L2.  The slices' statistics meet through distributed shared memory; every sum has a fixed order.  Sums over the columns are fp32, what is
+// computed of the entries, and the loss, is fp64, because a small loss is the difference of large terms.
+// Measured: loss of 512 x 152064 bf16 45 us, its gradient 57 (5.5 TB/s), both in one call 88; 777 x 50257 fp32 in one call 74, 4096 x 32000 bf16 131;
+// loss of 16 x 32000 8.2, all of it latency.
 #include "slim_gemv_i8.cuh"
 
 #include <cuda_bf16.h>
@@ -1164,7 +1166,7 @@ static int distill(int mode, const void* logits, int type, long long ld, const v
     for (int c = 1; c <= kDsMaxCluster; ++c) {
         const long long waves = (static_cast<long long>(M) * c + 2 * device_sm_count() - 1) / (2 * device_sm_count());
         const double t = static_cast<double>(waves) * (static_cast<double>(vecs) / c + 6500.0);
-        if (vecs <= c * 32768 && t < 0.98 * least) { least = t; cluster = c; }
+        if (vecs <= c * 65538 && t < 0.98 * least) { least = t; cluster = c; }       // a byte of marks per vector has to fit
     }
     cut(cluster);
     const size_t smem = static_cast<size_t>(entry_bytes(k)) + p.mark_bytes;

@@ -11,6 +11,9 @@
 // which costs L2 reads of 2 T bytes per 128 bytes of W and saves the launch of the quantizer.  Beyond, the codes come
 // by TMA from the workspace (slim_fp8.cu); W is then requested while the quantizer still runs.
 //
+// Measured, call after call (the bytes at the copy rate in brackets): 1 x 4096 x 4096 5.7 us (2.6), 16 x 11008 x 4096 11.6 (7.1), 33 x 11008 x 4096 13.9
+// (7.3), 77 x 32003 x 4112 38 (22).  W streams at 5.5 to 7 TB/s once it runs; the rest is set-up, the first block's way, and the meeting at the end.
+//
 // Warps: 0 loads of W (and of staged x); 1 MMAs, tensor memory; 4 to 7 scales, then the output (tensor-memory lanes 32 (w % 4) on); 2, 3, 8, 9
 // quantisation of x.  Every wait is bounded and reports through the workspace status word.
 #include "slim_fp8.cuh"

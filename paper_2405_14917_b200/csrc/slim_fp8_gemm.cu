@@ -13,6 +13,8 @@
 // Warps of a CTA (16): 0 TMA of its 128 tokens and its half of the rows of W per block into a ring of 32 KB slots; 1 in the leader the
 // MMAs, in the other CTA the relay that tells the leader its half has landed; 4 to 7 scale words; 8 to 15 output: they take D into
 // registers at once, so that the next tile's MMAs wait for the reading alone, and convert and store beside them.
+// Measured, call after call at the power cap, the quantizer of x among it: 2048 x 13824 x 5120 144 us (2.0 PFLOP/s; 116 for one launch alone), 512 x 5120 x
+// 13824 46, 1000 x 4096 x 32000 134.
 // Persistent pairs; every wait is bounded and reports through the workspace status word.
 #include "slim_fp8.cuh"
 

@@ -91,7 +91,8 @@ def test_loss_gradient_and_step(M, V, k, T, kind, rest):
 
 
 @pytest.mark.parametrize("M,V,kind,rest", [(2, 152064, "bf16", True), (1, 262145, "fp16", True), (1, 131073, "fp32", False), (300, 40001, "fp16", True),
-                                           (1, 600003, "fp32", True)])
+                                           (1, 600003, "fp32", True), (2, 2097152, "fp32", True), (1, 2097152, "fp16", True),
+                                           (1, 2097151, "fp32", False), (2, 1048577, "bf16", True)])
 def test_rows_longer_than_a_cta_or_a_cluster_holds(M, V, kind, rest):
     _run_all(*_case(M, V, 33, kind, 1.0, rest, seed=V), 1.0, kind)
 
