@@ -260,6 +260,25 @@ struct Slice {
     }
 };
 
+// An entry as it lies in memory, and what it says: its column (-1: absent) and the teacher's logit.
+__device__ __forceinline__ int2 raw_index(const DistillParams& p, size_t at) {
+    if (p.index64) return static_cast<const int2*>(p.index)[at];
+    return make_int2(static_cast<const int*>(p.index)[at], 0);
+}
+__device__ __forceinline__ int column_of(const DistillParams& p, int2 raw) {
+    const bool in = (!p.index64 || raw.y == 0) && raw.x >= 0 && raw.x < p.V;
+    return in ? raw.x : -1;
+}
+__device__ __forceinline__ uint32_t raw_value(const DistillParams& p, size_t at) {
+    if (p.value_type == SLIM_F32) return static_cast<const uint32_t*>(p.value)[at];
+    return static_cast<const unsigned short*>(p.value)[at];
+}
+__device__ __forceinline__ float teacher_logit(const DistillParams& p, uint32_t raw) {
+    if (p.value_type == SLIM_F32) return __uint_as_float(raw);
+    if (p.value_type == SLIM_F16) return __half2float(__ushort_as_half(static_cast<unsigned short>(raw)));
+    return __uint_as_float(raw << 16);
+}
+
 // Shared memory of k entries (a multiple of 16 bytes).
 __host__ __device__ __forceinline__ int entry_bytes(int k) { return (25 * k + 16 + 15) & ~15; }
 
@@ -286,25 +305,31 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     pdl_launch_dependents();
     pdl_wait();
 
+    // ---- the entries: columns, the teacher's values, the student's logits at them (wanted last, and fetched meanwhile).  The first 512
+    // are asked for before the row, behind which they would wait.
+    const size_t entry0 = static_cast<size_t>(row) * p.k;
+    int2 own_index = make_int2(-1, -1);
+    uint32_t own_value = 0;
+    if (tid < p.k) {
+        own_index = raw_index(p, entry0 + tid);
+        own_value = raw_value(p, entry0 + tid);
+    }
+    const float lse = REST ? p.lse[row] : 0.f;
     uint4 x[kDsVecs];
 #pragma unroll
     for (int u = 0; u < kDsVecs; ++u) x[u] = sl.load(tid + u * kDsThreads, MODE == kDsStep && sl.nv > kDsVecs * kDsThreads);
-
-    // ---- the entries: columns, the teacher's values, the student's logits at them (wanted last, and fetched meanwhile)
     float early = 0.f;
-    for (int j = tid; j < p.k; j += kDsThreads) {
-        const size_t at = static_cast<size_t>(row) * p.k + j;
-        const long long i = p.index64 ? static_cast<const long long*>(p.index)[at] : static_cast<const int*>(p.index)[at];
-        const bool in = i >= 0 && i < p.V;
-        double u;
-        if (p.value_type == SLIM_F32) u = static_cast<const float*>(p.value)[at];
-        else if (p.value_type == SLIM_F16) u = __half2float(static_cast<const __half*>(p.value)[at]);
-        else u = __bfloat162float(static_cast<const __nv_bfloat16*>(p.value)[at]);
-        s_idx[j] = in ? static_cast<int>(i) : -1;
-        const float sv = in ? DsType<T>::one(r_logits[i]) : 0.f;
-        if (j == tid) early = sv;
-        else s_s[j] = sv;
-        s_lq[j] = u * p.inv_t;
+    if (tid < p.k) {
+        const int i = column_of(p, own_index);
+        s_idx[tid] = i;
+        s_lq[tid] = static_cast<double>(teacher_logit(p, own_value)) * p.inv_t;
+        if (i >= 0) early = DsType<T>::one(r_logits[i]);
+    }
+    for (int j = tid + kDsThreads; j < p.k; j += kDsThreads) {
+        const int i = column_of(p, raw_index(p, entry0 + j));
+        s_idx[j] = i;
+        s_lq[j] = static_cast<double>(teacher_logit(p, raw_value(p, entry0 + j))) * p.inv_t;
+        s_s[j] = i >= 0 ? DsType<T>::one(r_logits[i]) : 0.f;
     }
     if (tid < 4) s_idx[p.k + tid] = -1;              // the search below reads whole quadruples
     if (REST)
@@ -333,7 +358,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
             if (s_idx[j] >= 0) { top = fmax(top, s_lq[j]); any = 1; finite |= !(s_lq[j] == -INFINITY); }
         any = __any_sync(0xffffffffu, any);
         double norm;
-        if (REST) norm = p.lse[row];
+        if (REST) norm = lse;
         else {
             any = __any_sync(0xffffffffu, finite);
             top = warp_max(top);
@@ -631,23 +656,6 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
         uint32_t f_val[AHEAD];
         float f_lse = 0.f, f_weight = 0.f;
         uint32_t* filter = reinterpret_cast<uint32_t*>(ds_smem + lay.filter + turn * kDsFilterBytes);
-        auto raw_index = [&](size_t at) {
-            if (p.index64) return static_cast<const int2*>(p.index)[at];
-            return make_int2(static_cast<const int*>(p.index)[at], 0);
-        };
-        auto column = [&](int2 raw) {                  // -1: absent
-            const bool in = (!p.index64 || raw.y == 0) && raw.x >= 0 && raw.x < p.V;
-            return in ? raw.x : -1;
-        };
-        auto raw_value = [&](size_t at) -> uint32_t {
-            if (p.value_type == SLIM_F32) return static_cast<const uint32_t*>(p.value)[at];
-            return static_cast<const unsigned short*>(p.value)[at];
-        };
-        auto teacher_logit = [&](uint32_t raw) {
-            if (p.value_type == SLIM_F32) return __uint_as_float(raw);
-            if (p.value_type == SLIM_F16) return __half2float(__ushort_as_half(static_cast<unsigned short>(raw)));
-            return __uint_as_float(raw << 16);
-        };
         auto fetch = [&](int row) {
             if (row >= p.M) return;
 #pragma unroll
@@ -656,8 +664,8 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                 const int j = lane + 32 * u;
                 const size_t at = static_cast<size_t>(row) * p.k + j;
                 if (j < p.k) {
-                    f_idx[u] = raw_index(at);
-                    f_val[u] = raw_value(at);
+                    f_idx[u] = raw_index(p, at);
+                    f_val[u] = raw_value(p, at);
                 }
             }
             if (REST) f_lse = p.lse[row];
@@ -691,7 +699,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             double u_t[AHEAD];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                idx[u] = lane + 32 * u < p.k ? column(f_idx[u]) : -1;
+                idx[u] = lane + 32 * u < p.k ? column_of(p, f_idx[u]) : -1;
                 if (idx[u] >= 0) g[u] = r_logits[idx[u]];
             }
             int seen = 0, columns = 0;
@@ -707,7 +715,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 if (lane + 32 * u < p.k) enter(lane + 32 * u, idx[u]);
-                u_t[u] = idx[u] >= 0 ? static_cast<double>(teacher_logit(f_val[u])) * p.inv_t : -INFINITY;
+                u_t[u] = idx[u] >= 0 ? static_cast<double>(teacher_logit(p, f_val[u])) * p.inv_t : -INFINITY;
             }
             const float lse = f_lse, weight = f_weight;
             fetch(row + 2 * stride);
@@ -716,8 +724,8 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
 #pragma unroll 1
             for (int j = lane + 32 * AHEAD; j < p.k; j += 32) {
                 const size_t at = static_cast<size_t>(row) * p.k + j;
-                const int i = column(raw_index(at));
-                const double u = i >= 0 ? static_cast<double>(teacher_logit(raw_value(at))) * p.inv_t : -INFINITY;
+                const int i = column_of(p, raw_index(p, at));
+                const double u = i >= 0 ? static_cast<double>(teacher_logit(p, raw_value(p, at))) * p.inv_t : -INFINITY;
                 enter(j, i);
                 s_s[j] = i >= 0 ? DsType<T>::one(r_logits[i]) : 0.f;
                 s_lq[j] = u;
