@@ -13,8 +13,8 @@
 // Warps of a CTA (16): 0 TMA of its 128 tokens and its half of the rows of W per block into a ring of 32 KB slots; 1 in the leader the
 // MMAs, in the other CTA the relay that tells the leader its half has landed; 4 to 7 scale words; 8 to 15 output: they take D into
 // registers at once, so that the next tile's MMAs wait for the reading alone, and convert and store beside them.
-// Measured, call after call at the power cap, the quantizer of x among it: 2048 x 13824 x 5120 144 us (2.0 PFLOP/s; 116 for one launch alone), 512 x 5120 x
-// 13824 46, 1000 x 4096 x 32000 134.
+// Measured, call after call at the power cap, the quantizer of x among it: 2048 x 13824 x 5120 139 us (2.1 PFLOP/s at 1.25 GHz), 512 x 5120 x 13824 46,
+// 1000 x 4096 x 32000 137.
 // Persistent pairs; every wait is bounded and reports through the workspace status word.
 #include "slim_fp8.cuh"
 
@@ -199,38 +199,53 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
                     if (++s == kFgStages) { s = 0; ph ^= 1u; }
                 }
         } else if (warp >= 4) {
-            // ---- scale words: this warp's quarter of the lanes, of all of the CTA's tokens and the tile's features
+            // ---- scale words: this warp's quarter of the lanes, of all of the CTA's tokens and the tile's features.  A group's are fetched while
+            // the one before is written: lane l reads W's scale of column l / 4 (32 features, which lie in one block of 128), block g + l % 4.
             const int q = warp & 3;
             const uint32_t sf_t = tmem + kFgColScales + (static_cast<uint32_t>(32 * q) << 16);
             const uint32_t sf_full_leader = fg::map_to_cta(sf_full(0), 0);
             const int n_blocks = (p.N + 127) / 128;
-            bool ok = true;
-            for (int tile = pair; tile < p.tiles && ok; tile += pairs) {
-                const int m0 = min(tile % p.tok_tiles * kFgTok + 128 * rank, p.Mp - 128), nb0 = tile / p.tok_tiles * feat;
-                for (int g = 0; g < G; g += 4, ++issued) {
-                    const int b = issued & 1;
-                    uint32_t xw[4], ww[8];
+            struct Words { uint32_t x[4], w; };
+            auto fetch = [&](int tile, int g, Words& v) {
+                const int m0 = min(tile % p.tok_tiles * kFgTok + 128 * rank, p.Mp - 128), n = tile / p.tok_tiles * feat + 32 * (lane >> 2);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) xw[c] = __ldcg(p.x_scales + static_cast<size_t>(g >> 2) * p.Mp + m0 + 32 * c + lane);
+                for (int c = 0; c < 4; ++c) v.x[c] = __ldcg(p.x_scales + static_cast<size_t>(g >> 2) * p.Mp + m0 + 32 * c + lane);
+                v.w = __float_as_uint(__ldg(p.scales + static_cast<size_t>(min(n >> 7, n_blocks - 1)) * G + min(g + (lane & 3), G - 1)));
+            };
+            auto put = [&](const Words& v) {
+                const int b = issued & 1;
+                uint32_t own = (v.w >> 23 & 0xffu) << (8 * (lane & 3)), ww[8];
+                own |= __shfl_xor_sync(0xffffffffu, own, 1);
+                own |= __shfl_xor_sync(0xffffffffu, own, 2);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {      // 32 features of column c lie in one block of 128
-                        const float* sw = p.scales + static_cast<size_t>(min((nb0 + 32 * c) >> 7, n_blocks - 1)) * G + g;
-                        uint32_t v = 0;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (g + e < G) v |= (__float_as_uint(__ldg(sw + e)) >> 23 & 0xffu) << (8 * e);
-                        ww[c] = v;
-                    }
-                    ok = tc::warp_wait(sf_empty(b), ((issued >> 1) & 1u) ^ 1u, abort);
-                    if (!ok) break;
-                    tc::fence_after();
-                    fg::st4(sf_t + kFgScaleCols * b, xw);
-                    tc::st8(sf_t + kFgScaleCols * b + 4, ww);
-                    tc::wait_st();
-                    tc::fence_before();
-                    __syncwarp();
-                    if (lane == 0) fg::arrive_cluster(sf_full_leader + 8u * b);
-                }
+                for (int c = 0; c < 8; ++c) ww[c] = __shfl_sync(0xffffffffu, own, 4 * c);
+                if (!tc::warp_wait(sf_empty(b), ((issued >> 1) & 1u) ^ 1u, abort)) return false;
+                tc::fence_after();
+                fg::st4(sf_t + kFgScaleCols * b, v.x);
+                tc::st8(sf_t + kFgScaleCols * b + 4, ww);
+                tc::wait_st();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) fg::arrive_cluster(sf_full_leader + 8u * b);
+                ++issued;
+                return true;
+            };
+            int tile = pair, g = 0;                    // of the group fetched last
+            auto next = [&] {
+                g += 4;
+                if (g >= G) { g = 0; tile += pairs; }
+                return tile < p.tiles;
+            };
+            Words even, odd;
+            bool more = tile < p.tiles;
+            if (more) fetch(tile, g, even);
+            while (more) {
+                more = next();
+                if (more) fetch(tile, g, odd);
+                if (!put(even) || !more) break;
+                more = next();
+                if (more) fetch(tile, g, even);
+                if (!put(odd)) break;
             }
         }
     } else {
@@ -308,15 +323,17 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
 }
 
 // ------------------------------------------------------------------------------------------ host side
-// Features of a tile: a multiple of 32.  The MMAs of a block take twice as many cycles as there are features, and a block no less than 330 however few
-// (the issuing warp's turn); with one buffer for D, 256 features, a tile waits for the one before it to be read.
+// Features of a tile: a multiple of 32.  Measured in cycles of the issuing warp: a block takes its MMAs' time, 2.05 per feature, or 390 however few
+// features (that warp's turn), and a tile 2400 beside its blocks (reading D slows the next tile's MMAs), 3100 where there is one D (256 features).
+// 2048 x 13824 x 5120 comes to 145000 at 256, 224 and 192 alike (138, 137 and 139 us); 512 x 5120 x 13824 at 256 / 192 / 160 took 49.5 / 45.1 / 44.3 us, 1024 x 11008 x
+// 4096 at 256 / 224 / 160 53.6 / 50.3 / 51.9.  Equal, wider tiles read less.
 static int fg_features(int tok_tiles, int N, int G, int pairs) {
     int best = kFgFeat;
     double least = 1e30;
     for (int feat = kFgFeat; feat >= 64; feat -= 32) {
         const long long tiles = static_cast<long long>(tok_tiles) * ((N + feat - 1) / feat), waves = (tiles + pairs - 1) / pairs;
-        const double t = static_cast<double>(waves) * (G * (feat > 165 ? 2.0 * feat : 330.0) + (feat > kFgFeatTwice ? 800.0 : 0.0));
-        if (t < 0.99 * least) { least = t; best = feat; }
+        const double t = static_cast<double>(waves) * (G * (feat > 190 ? 2.05 * feat : 390.0) + (feat > kFgFeatTwice ? 3100.0 : 2400.0));
+        if (t < 0.995 * least) { least = t; best = feat; }
     }
     return best;
 }
