@@ -421,7 +421,7 @@ int slim_gptq_quantize(const void* W, const void* x, const uint8_t* bits_host, d
  *   [ceil(N/128)][ceil(K/128)]. */
 int slim_fp8_quantize(const void* W, int type, long long ld, void* codes, float* scales, int N, int K, void* stream);
 
-/* Host-only: workspace of slim_fp8_linear for these shapes: the header (and flags) of slim_workspace_bytes, then, beyond 32 tokens, the codes
+/* Host-only: workspace of slim_fp8_linear for these shapes: the header (and flags) of slim_workspace_bytes, then, beyond 16 tokens, the codes
  * and scales of x.  One of the larger size may be shared with the other linear layers' calls on one stream (initialised by slim_workspace_init). */
 int slim_fp8_workspace_bytes(int M, int N, int K, size_t* out_bytes);
 

@@ -198,5 +198,6 @@ bool fp8_few_takes_x(int M);                       // quantises x itself
 cudaError_t fp8_few(const Fp8Args& a);
 cudaError_t fp8_gemm(const Fp8Args& a);
 bool fp8_use_gemm(int M, int N, int K);
+double fp8_few_cycles(int M, int N, int K);
 
 }  // namespace slim

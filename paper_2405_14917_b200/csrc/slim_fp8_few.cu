@@ -7,8 +7,9 @@
 // r / 32, the same in all lane quarters) into a buffer per slot.  At the end the CTAs of a cluster add their sums through
 // distributed shared memory, every CTA a share of the tokens, in rank order: no workspace, no second kernel, one result.
 //
-// Up to 32 tokens x is quantised here (TAKES_X), by four warps that take the blocks in turn, from x itself: every CTA does it for its part of K,
-// which costs L2 reads of 2 T bytes per 128 bytes of W and saves the launch of the quantizer.  Beyond, the codes come
+// Up to 16 tokens x is quantised here (TAKES_X), by four warps that take the blocks in turn, from x itself: every CTA does it for its part of K,
+// which costs L2 reads of 2 T bytes per 128 bytes of W and saves the launch of the quantizer (us, here / by the quantizer: 4096 x 4096 at 1 and 16
+// tokens 6.2 / 7.3 and 7.7 / 8.1, 32000 x 4096 24.2 / 25.9 and 24.3 / 25.8; at 32 tokens 9.5 / 8.7 and 31.8 / 26.1).  Beyond, the codes come
 // by TMA from the workspace (slim_fp8.cu); W is then requested while the quantizer still runs.
 //
 // Measured, call after call (the bytes at the copy rate in brackets): 1 x 4096 x 4096 5.7 us (2.6), 16 x 11008 x 4096 11.6 (7.1), 33 x 11008 x 4096 13.9
@@ -26,11 +27,10 @@ constexpr int kFewXWarps = 4;
 constexpr int kFewMaxCluster = 8;
 
 template <int T> struct FewCfg {
-    static constexpr bool TAKES_X = T <= 32;
+    static constexpr bool TAKES_X = T <= 16;
     static constexpr int THREADS = TAKES_X ? 320 : 256;
     static constexpr int W_BYTES = 128 * 128, X_BYTES = T * 128;
     static constexpr int STAGES = T <= 16 ? 5 : T <= 32 ? 4 : 3;
-    static constexpr int XSHARE = T / 16;                                 // warps that quantise a block together, 16 tokens each
     static constexpr bool OWN_RECV = T <= 64;                             // the others' sums have a place of their own, not the ring's
     static constexpr int COL_SF = T;                                      // tensor memory: D, then per slot 4 columns of W's scales and T / 32 of x's
     static constexpr int TMEM_USED = T + 8 * STAGES;
@@ -91,7 +91,7 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
         *abort = 0;
         for (int s = 0; s < C::STAGES; ++s) {
             sb::init(w_full(s), 1);
-            sb::init(x_full(s), C::XSHARE);
+            sb::init(x_full(s), 1);
             sb::init(sf_full(s), 4);
             sb::init(empty(s), 1);
         }
@@ -214,21 +214,21 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             if (++s == C::STAGES) { s = 0; ph ^= 1u; }
         }
     } else if (C::TAKES_X) {
-        // ---- x into codes: half a warp per token and block, two tokens of a warp at a time, a block in kFewXWarps / XSHARE per group of warps
-        const int xw = warp < 4 ? warp - 2 : warp - 6, part = xw % C::XSHARE;
-        constexpr int TURNS = kFewXWarps / C::XSHARE;
-        static_assert(TURNS <= C::STAGES, "the first blocks of the warps have slots of their own");
+        // ---- x into codes: half a warp per token and block, two tokens of a warp at a time, one block in four
+        const int xw = warp < 4 ? warp - 2 : warp - 6;
+        constexpr int TURNS = kFewXWarps;
+        static_assert(!C::TAKES_X || TURNS <= C::STAGES, "the first blocks of the warps have slots of their own");
         const int half = lane >> 4, c = lane & 15;
         const X* x = static_cast<const X*>(p.x) + static_cast<size_t>(m0) * p.ldx;
         uint4 v[8];
         auto fetch = [&](int i) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const int t = 16 * part + 2 * u + half, k = 128 * (g0 + i) + 8 * c;
+                const int t = 2 * u + half, k = 128 * (g0 + i) + 8 * c;
                 v[u] = i < steps && t < tokens && k < p.K ? __ldg(reinterpret_cast<const uint4*>(x + static_cast<size_t>(t) * p.ldx + k)) : make_uint4(0, 0, 0, 0);
             }
         };
-        int s = xw / C::XSHARE;                        // below the number of slots
+        int s = xw;
         uint32_t ph = 0;
         fetch(s);
         for (int i = s; i < steps; i += TURNS) {
@@ -238,7 +238,7 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
             uint32_t e[8];
             auto put = [&](int u) {
                 // row t of a swizzled tile: its 16-byte chunks stand at chunk ^ (t & 7)
-                const int t = 16 * part + 2 * u + half;
+                const int t = 2 * u + half;
                 const uint32_t at = s_x + s * C::X_BYTES + t * 128 + ((((c >> 1) ^ (t & 7)) << 4) | ((c & 1) << 3));
                 asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(at), "r"(codes[u].x), "r"(codes[u].y) : "memory");
                 if (c == 0) smem[C::OFF_SX + s * T + t] = static_cast<uint8_t>(e[u]);
@@ -390,7 +390,13 @@ static cudaError_t few_by_tokens(const Fp8Args& a) {
     if (a.M <= 64) return few_launch<64, X>(a);
     return few_launch<128, X>(a);
 }
-bool fp8_few_takes_x(int M) { return M <= 32; }
+bool fp8_few_takes_x(int M) { return M <= 16; }
+// Cycles from 65 tokens on: a block of a CTA takes 1300 (its W, two CTAs per SM, at HBM's rate), a CTA 9000 beside its blocks.
+double fp8_few_cycles(int M, int N, int K) {
+    const long long tiles = static_cast<long long>((N + 127) / 128) * ((M + 127) / 128);
+    const int G = (K + f8::kBlock - 1) / f8::kBlock, slots = 2 * device_sm_count(), c = few_cluster(tiles, G, slots);
+    return static_cast<double>((tiles * c + slots - 1) / slots) * ((G + c - 1) / c * 1300.0 + 9000.0);
+}
 cudaError_t fp8_few(const Fp8Args& a) { return a.x_type == SLIM_F16 ? few_by_tokens<__half>(a) : few_by_tokens<__nv_bfloat16>(a); }
 
 }  // namespace slim

@@ -327,7 +327,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
 // features (that warp's turn), and a tile 2400 beside its blocks (reading D slows the next tile's MMAs), 3100 where there is one D (256 features).
 // 2048 x 13824 x 5120 comes to 145000 at 256, 224 and 192 alike (138, 137 and 139 us); 512 x 5120 x 13824 at 256 / 192 / 160 took 49.5 / 45.1 / 44.3 us, 1024 x 11008 x
 // 4096 at 256 / 224 / 160 53.6 / 50.3 / 51.9.  Equal, wider tiles read less.
-static int fg_features(int tok_tiles, int N, int G, int pairs) {
+static int fg_features(int tok_tiles, int N, int G, int pairs, double* cycles) {
     int best = kFgFeat;
     double least = 1e30;
     for (int feat = kFgFeat; feat >= 64; feat -= 32) {
@@ -335,6 +335,7 @@ static int fg_features(int tok_tiles, int N, int G, int pairs) {
         const double t = static_cast<double>(waves) * (G * (feat > 190 ? 2.05 * feat : 390.0) + (feat > kFgFeatTwice ? 3100.0 : 2400.0));
         if (t < 0.995 * least) { least = t; best = feat; }
     }
+    *cycles = least;
     return best;
 }
 
@@ -355,16 +356,22 @@ cudaError_t fp8_gemm(const Fp8Args& a) {
     p.y_type = a.y_type; p.M = a.M; p.N = a.N; p.G = (a.K + f8::kBlock - 1) / f8::kBlock; p.Mp = a.Mp;
     p.tok_tiles = (a.M + kFgTok - 1) / kFgTok;
     const int pairs = device_sm_count() / 2;
-    p.feat = fg_features(p.tok_tiles, a.N, p.G, pairs);
+    double cycles = 0.0;
+    p.feat = fg_features(p.tok_tiles, a.N, p.G, pairs, &cycles);
     p.tiles = p.tok_tiles * ((a.N + p.feat - 1) / p.feat);
     CUtensorMap x_map, w_map;
     if (!make_byte_map(&x_map, a.x_codes, a.M, a.K, 128) || !make_byte_map(&w_map, a.codes, a.N, a.K, p.feat / 2)) return cudaErrorUnknown;
     PdlLaunch l(static_cast<unsigned>(2 * (p.tiles < pairs ? p.tiles : pairs)), kFgThreads, kFgSmem, a.stream);      // clusters of 2: see the kernel
     return cudaLaunchKernelEx(&l.cfg, fp8_gemm_kernel, x_map, w_map, p);
 }
+// Up to 128 tokens the other kernel, which cuts K; beyond, whichever is expected to end first: that one also at 129 to 256 tokens of narrow and deep layers,
+// whose few tiles walk all of K here.  (us, that one / this one: 4096 x 11008 at 65, 128, 256 and 300 tokens 16.4 / 25.9, 18.9 / 27.2, 24.2 / 28.5, 35.3 / 30.6;
+// 11008 x 4096 17.2 / 17.1, 20.0 / 20.0, 34.7 / 20.7; 32000 x 4096 28.7 / 34.6, 29.7 / 36.3, 52.7 / 38.6.)
 bool fp8_use_gemm(int M, int N, int K) {
-    (void)N; (void)K;
-    return M > 128;
+    if (M <= 128) return false;
+    double cycles = 0.0;
+    fg_features((M + kFgTok - 1) / kFgTok, N, (K + f8::kBlock - 1) / f8::kBlock, device_sm_count() / 2, &cycles);
+    return cycles + 4000.0 <= fp8_few_cycles(M, N, K);
 }
 
 }  // namespace slim
