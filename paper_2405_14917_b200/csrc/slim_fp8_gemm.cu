@@ -4,8 +4,8 @@
 // tensor-memory lane is a token) times up to 256 rows of W (half from each CTA's shared memory) over 32 columns.  All scales are powers of two, so the
 // block-scaled form (kind::mxf8f6f4, E8M0 scales of 32 columns each) applies them inside the MMA: the four MMAs of a block of 128 columns name the
 // same byte of a row's scale word, and a tile's sum over all of K stays in tensor memory.  Plain MMAs with a pass over D per block (into
-// registers, under the block's scale) reached 2.1 PFLOP/s at 2048 x 13824 x 5120 in the best of four forms: reading D competes with
-// the MMAs' own accumulation (430 to 550 cycles per block beside them, 150 alone, of 512 that its MMAs take).
+// registers, under the block's scale) took 139 us at 2048 x 13824 x 5120 in the best of four forms where this takes 122 (both in short runs): reading D
+// competes with the MMAs' own accumulation (430 to 550 cycles per block beside them, 150 alone, of 512 that its MMAs take).
 //
 // Scale words (four blocks' bytes) go to tensor memory by tcgen05.st: row r's word at lane r % 32 of column r / 32, the same in all four lane
 // quarters; two buffers.  A CTA has the words of its own tokens and of all features.
