@@ -330,7 +330,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
 static int fg_features(int tok_tiles, int N, int G, int pairs, double* cycles) {
     int best = kFgFeat;
     double least = 1e30;
-    for (int feat = kFgFeat; feat >= 64; feat -= 32) {
+    for (int feat = kFgFeat; feat >= 160; feat -= 32) {
         const long long tiles = static_cast<long long>(tok_tiles) * ((N + feat - 1) / feat), waves = (tiles + pairs - 1) / pairs;
         const double t = static_cast<double>(waves) * (G * (feat > 190 ? 2.05 * feat : 390.0) + (feat > kFgFeatTwice ? 3100.0 : 2400.0));
         if (t < 0.995 * least) { least = t; best = feat; }

@@ -85,6 +85,20 @@ def test_linear(M, N, K, kind, out):
     _check(y, x, layer.codes, layer.scales)
 
 
+@pytest.mark.parametrize("M,N,K", [(1000, 9000, 272), (1024, 11008, 528), (700, 9000, 1040), (600, 7001, 2064), (300, 11600, 1040),
+                                   (600, 500, 4112), (200, 4096, 11008), (130, 1023, 8192)])
+def test_several_tiles(M, N, K):
+    """More tiles than CTA pairs, at each width that a tile may have (256 features, with one accumulator, 224, 192, 160), ragged last ones; and narrow
+    and deep layers of more tokens than one tile of the kernel that cuts K."""
+    slim = _slim()
+    layer = slim.Fp8Linear.from_weight(_weight(N, K, N, "bf16").cuda())
+    x = _x(M, K, M, "bf16").cuda()
+    ws = layer.new_workspace(M)
+    y = layer.forward(x, ws)
+    slim.workspace_status(ws)
+    _check(y, x, layer.codes, layer.scales)
+
+
 @pytest.mark.parametrize("M", [3, 40, 200])
 def test_scales_of_every_block_count(M):
     """Scales that differ by many powers of two from block to block, and others than the quantizer would give: each block under its own."""
