@@ -39,7 +39,7 @@ struct DistillParams {
     const float* lse;        // [M], or null: the teacher is renormalised over its entries
     const float* dloss;      // [M]
     float* loss;             // [M]
-    float* saved;            // [M][4]: the row's maximum, its sum of exponentials, that of the columns outside the set, 0
+    float* saved;            // [M][4]: the largest logit outside the set, the row's sum of exponentials, that outside the set relative to the first, 0
     void* grad;
     long long ld, ldg;       // row strides in elements
     float c;                 // log2(e) / T
@@ -52,6 +52,16 @@ struct DistillParams {
 };
 
 // ------------------------------------------------------------------------------------------ element types
+template <uint32_t NINF2>
+__device__ __forceinline__ void ds_hide16(uint4& v, uint32_t b) {
+    uint32_t* w[4] = {&v.x, &v.y, &v.z, &v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                      // bit 2i as the sign of a byte 0, bit 2i + 1 of a byte 1, spread over a half each
+        uint32_t m;
+        asm("prmt.b32 %0, %1, %2, 0xdd88;" : "=r"(m) : "r"(b << (7 - 2 * i)), "r"(b << (14 - 2 * i)));
+        *w[i] = (*w[i] & ~m) | (NINF2 & m);
+    }
+}
 template <typename T> struct DsType;
 template <> struct DsType<float> {
     static constexpr int E = 4;
@@ -60,6 +70,11 @@ template <> struct DsType<float> {
     }
     static __device__ __forceinline__ uint4 pack(const float* f) {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+    // elements whose bit is set become minus infinity
+    static __device__ __forceinline__ void hide(uint4& v, uint32_t b) {
+        constexpr uint32_t NINF = 0xff800000u;
+        v.x = b & 1u ? NINF : v.x; v.y = b & 2u ? NINF : v.y; v.z = b & 4u ? NINF : v.z; v.w = b & 8u ? NINF : v.w;
     }
     static __device__ __forceinline__ float one(float v) { return v; }
     static __device__ __forceinline__ float round(float v) { return v; }
@@ -80,6 +95,7 @@ template <> struct DsType<__half> {
         for (int i = 0; i < 4; ++i) { const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    static __device__ __forceinline__ void hide(uint4& v, uint32_t b) { ds_hide16<0xfc00fc00u>(v, b); }
     static __device__ __forceinline__ float one(__half v) { return __half2float(v); }
     static __device__ __forceinline__ __half round(float v) { return __float2half_rn(v); }
 };
@@ -96,6 +112,7 @@ template <> struct DsType<__nv_bfloat16> {
         for (int i = 0; i < 4; ++i) { const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t*>(&h); }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
+    static __device__ __forceinline__ void hide(uint4& v, uint32_t b) { ds_hide16<0xff80ff80u>(v, b); }
     static __device__ __forceinline__ float one(__nv_bfloat16 v) { return __bfloat162float(v); }
     static __device__ __forceinline__ __nv_bfloat16 round(float v) { return __float2bfloat16_rn(v); }
 };
@@ -151,25 +168,34 @@ __device__ __forceinline__ float rcp(float v) {      // within an ulp
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// What a row's sums come to: R outside the set and z of the set's columns (all of it in R without the rest), and the teacher's listed
-// mass, that of the rest (0 without it) and both together.
+// What a row's sums come to: R outside the set, relative to m, the largest logit there (all of the row without the rest), and z of the set's columns,
+// relative to `top`, the largest of them; and the teacher's listed mass, that of the rest (0 without it) and both together.  R has a maximum of its own
+// because the student may leave the rest next to nothing: relative to the row's maximum it would be nothing from a distance of 87 T on.
 struct RowTerms {
-    float ref, R, Z, p_in;   // the row's maximum (0 if that is minus infinity); Z = R + z; the set's mass
+    float ref, Z;            // the row's maximum (0 if that is minus infinity), the sum of all columns relative to it
+    float m, R;
+    float p_in;              // the set's mass
     float inv_z, factor;     // of 2^((s - ref) c) in the gradient of the columns outside the set, but for the row's weight
 };
 template <bool REST>
-__device__ __forceinline__ RowTerms row_terms(float m, float R, float z, float q_sum, float q_rest, float mass) {
+__device__ __forceinline__ RowTerms row_terms(float c, float m, float R, float top, float z, float q_sum, float q_rest, float mass) {
     RowTerms t;
-    t.ref = m == -INFINITY ? 0.f : m;
-    t.R = REST && R < 1.17549435e-38f ? 0.f : R;     // below fp32's normal range there is nothing
-    t.Z = t.R + z;
+    const float most = REST ? fmaxf(m, top) : m;
+    t.ref = most == -INFINITY ? 0.f : most;
+    t.m = m;
+    t.R = R;
+    const float r = REST ? R * ex2((m - t.ref) * c) : R;
+    z = REST ? z * ex2((top - t.ref) * c) : 0.f;
+    t.Z = r + z;
     const float over = rcp(t.Z);
     t.inv_z = t.Z == 0.f ? 0.f : over;
     t.p_in = z * t.inv_z;
     t.factor = mass * t.inv_z;
-    // p (1 - q'/p') = 2^.. (p' - q') / (p' Z), where p' is what the set leaves of 1, or R / Z where that would cancel
-    if (REST && !(q_rest == 0.f))
-        t.factor = t.Z == 0.f || t.R == 0.f ? 0.f : t.p_in < 0.5f ? (q_sum - t.p_in) * rcp(1.f - t.p_in) * over : (t.R * over - q_rest) * rcp(t.R);
+    // p (1 - q'/p') = 2^.. (p' - q') / (p' Z), where p' is what the set leaves of 1, or r / Z where that would cancel
+    if (REST && !(q_rest == 0.f)) {
+        const bool none = r < 1.17549435e-38f && t.Z == t.Z;        // below fp32's normal range there is nothing; a NaN in the set goes through
+        t.factor = t.Z == 0.f || none ? 0.f : t.p_in < 0.5f ? (q_sum - t.p_in) * rcp(1.f - t.p_in) * over : (r * over - q_rest) * rcp(r);
+    }
     return t;
 }
 // e^x in 64 bits for x up to a few (a log-probability), within 1e-14 of its value: x = n ln 2 + r after Cody and Waite (ln 2 = 355 / 512 and a
@@ -187,6 +213,11 @@ __device__ __forceinline__ double exp_log(double x) {
     const double ab = fma(b, r2, a), cd = fma(d, r2, c), ef = fma(f, r2, e);
     const double y = fma(fma(ef, r4, cd), r4, ab);
     return __hiloint2double(__double2hiint(y) + (static_cast<int>(n) << 20), __double2loint(y));
+}
+__device__ __forceinline__ float redux_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
@@ -219,8 +250,8 @@ __device__ __forceinline__ double row_loss(const RowTerms& t, double q_rest, int
     l = warp_sum(l);
     if (REST && !(q_rest == 0.0)) {
         p_in = warp_sum(p_in);
-        const double lr = __shfl_sync(0xffffffffu, v, 2) - lz;
-        l += q_rest * (__shfl_sync(0xffffffffu, v, 1) - (t.Z == 0.f || t.R == 0.f ? -INFINITY : p_in < 0.5 ? log(1.0 - p_in) : lr));
+        const double lr = (static_cast<double>(t.m) - static_cast<double>(t.ref)) * cd * ln2 + __shfl_sync(0xffffffffu, v, 2) - lz;
+        l += q_rest * (__shfl_sync(0xffffffffu, v, 1) - (t.Z == 0.f || (t.R == 0.f && t.Z == t.Z) ? -INFINITY : p_in < 0.5 ? log(1.0 - p_in) : lr));
     }
     return l;
 }
@@ -393,6 +424,19 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint4* xh = x + HALF * h;
+                if (REST) {                            // the listed columns take no part; their gradient is written apart
+                    uint32_t b[HALF], some = 0;
+#pragma unroll
+                    for (int u = 0; u < HALF; ++u) {
+                        const int j = j0 + tid + (HALF * h + u) * kDsThreads;
+                        b[u] = j < sl.nv ? mark[j] : 0u;
+                        some |= b[u];
+                    }
+                    if (some != 0) {
+#pragma unroll
+                        for (int u = 0; u < HALF; ++u) DsType<T>::hide(xh[u], b[u]);
+                    }
+                }
                 const float cm = vec_max<HALF>(xh, static_cast<const T*>(nullptr));
                 if (cm > tm) { ts *= tm == -INFINITY ? 0.f : ex2((tm - cm) * p.c); tm = cm; }
                 const float neg = tm == -INFINITY ? 0.f : -tm;
@@ -405,14 +449,6 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
                     if (j < sl.nv) {
                         float f[E];
                         DsType<T>::unpack(xh[u], f);
-                        if (REST) {
-                            const uint32_t b = mark[j];
-                            if (b != 0) {
-#pragma unroll
-                                for (int e = 0; e < E; ++e)
-                                    if (b >> e & 1u) f[e] = -INFINITY;
-                            }
-                        }
 #pragma unroll
                         for (int e = 0; e < E; e += 2) {
                             float a, b;
@@ -465,19 +501,22 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     const double q_sum = s_row[0];
     const bool any = s_row[1] != 0.0;
     double q_rest = 0.0;
-    float z = 0.f;
+    float z = 0.f, top = -INFINITY;
     if (REST) {
-        const float ref = m == -INFINITY ? 0.f : m;
         int columns = 0;
         for (int j = lane; j < p.k; j += 32)
-            if (s_first[j]) { z += ex2((s_s[j] - ref) * p.c); ++columns; }
+            if (s_first[j]) { top = fmaxf(top, s_s[j]); ++columns; }
+        top = redux_max(top);
+        const float ref = top == -INFINITY ? 0.f : top;
+        for (int j = lane; j < p.k; j += 32)
+            if (s_first[j]) z += ex2((s_s[j] - ref) * p.c);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
         columns = static_cast<int>(__reduce_add_sync(0xffffffffu, columns));
         if (columns < p.V) q_rest = q_sum >= 1.0 ? 0.0 : 1.0 - q_sum;         // NaN stays NaN
     }
     const double mass = q_sum + q_rest;
-    const RowTerms t = row_terms<REST>(m, static_cast<float>(R), z, static_cast<float>(q_sum), static_cast<float>(q_rest), static_cast<float>(mass));
+    const RowTerms t = row_terms<REST>(p.c, m, static_cast<float>(R), top, z, static_cast<float>(q_sum), static_cast<float>(q_rest), static_cast<float>(mass));
     // loss, in 64 bits, by the warp that is given it (below, beside the gradient)
     auto write_loss = [&] {
         const double l = row_loss<REST>(t, q_rest, p.k, p.c, s_q, s_lq, s_idx, s_s, s_first, lane);
@@ -557,7 +596,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
 // ------------------------------------------------------------------------------------------ the one pass over many rows
 // With more rows than CTAs at once, a CTA (or cluster) takes row after row, and what a row waits for is done for later ones meanwhile, by two warps beside
 // the sixteen that take the rows in turn: they have a row brought into shared memory (one bulk copy), read its entries and the logits at them two
-// rows ahead, work out the teacher's probabilities, mark the listed columns, and when the sixteen have the row's statistics compute its loss beside their
+// rows ahead, work out the teacher's probabilities, and when the sixteen have the row's statistics compute its loss beside their
 // gradient.  (One such warp was what all waited for: it runs some 700 instructions per row, alone in its code and at an instruction in 20 cycles.)
 // The sixteen take the row from shared memory into registers at once, which frees the buffer for the next.  4096 x 32000 bf16 took 173 us with
 // a CTA per row (of 22000 cycles 9000 went until the entries were there and 4000 into the row's own terms), two per SM.
@@ -576,13 +615,12 @@ constexpr int kDsEntryBufs = 4;
 
 template <typename T>
 struct RowsSmem {            // byte offsets
-    int row, filter, entries, entry_stride, mark, total;
-    __host__ __device__ RowsSmem(int slice, int k, int mark_bytes) {
+    int row, filter, entries, entry_stride, total;
+    __host__ __device__ RowsSmem(int slice, int k) {
         row = 0;
         filter = (slice / DsType<T>::E + 1) * 16;
         entries = filter + 2 * kDsFilterBytes;         // one for each of the two warps
-        mark = entry_bytes(k);
-        entry_stride = mark + (mark_bytes + 15) / 16 * 16;
+        entry_stride = entry_bytes(k);
         total = entries + kDsEntryBufs * entry_stride;
     }
 };
@@ -596,17 +634,12 @@ __device__ __forceinline__ uint32_t map_cluster(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float redux_max(float v) {
-    float r;
-    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-    return r;
-}
 
 template <typename T, bool REST, int MODE>
 __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const DistillParams p) {
     constexpr int E = DsType<T>::E;
     extern __shared__ __align__(16) unsigned char ds_smem[];
-    const RowsSmem<T> lay(p.slice, p.k, p.mark_bytes);
+    const RowsSmem<T> lay(p.slice, p.k);
     __shared__ __align__(8) uint64_t s_bar[2 + 3 * kDsEntryBufs + 2];
     __shared__ float2 s_part[2][kDsWarps];
     __shared__ float2 s_slice[2][kDsMaxCluster];
@@ -637,7 +670,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
         for (int b = 0; b < 2; ++b) sb::init(slice_full(b), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    for (int i = tid; i < (lay.total - lay.filter) / 16; i += kDsRowsThreads)      // the filters and the marks are zero between rows
+    for (int i = tid; i < (lay.entries - lay.filter) / 16; i += kDsRowsThreads)    // the filters are zero between rows
         reinterpret_cast<uint4*>(ds_smem + lay.filter)[i] = make_uint4(0, 0, 0, 0);
     __syncthreads();
     if (ranks > 1) cluster_sync_all();                 // the others' barriers exist
@@ -679,20 +712,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             int* s_idx = reinterpret_cast<int*>(s_lq + p.k);
             float* s_s = reinterpret_cast<float*>(s_idx + p.k + 4);
             uint8_t* s_first = reinterpret_cast<uint8_t*>(s_s + p.k);
-            uint32_t* s_mark = reinterpret_cast<uint32_t*>(e0 + lay.mark);
             const T* r_logits = logits + static_cast<long long>(row) * p.ld;
-            const int shift = slice_of(row).shift - v0;
-            auto mark_word = [&](int i, int sh) { return s_mark + ((i + sh) / E >> 2); };
-            // the marks of the row that had this buffer go
-            if (REST && n >= kDsEntryBufs) {
-                const int old = slice_of(row - kDsEntryBufs * stride).shift - v0;
-#pragma unroll 2
-                for (int j = lane; j < p.k; j += 32) {
-                    const int i = s_idx[j];
-                    if (i >= v0 && i < v1) *mark_word(i, old) = 0u;
-                }
-                __syncwarp();
-            }
             // the first 64 entries in registers, two of a lane side by side; the others after them
             T g[AHEAD];
             int idx[AHEAD];
@@ -709,7 +729,6 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                 if (i >= 0) {
                     ++columns;
                     seen |= atomicOr(filter + (i >> 5 & (kDsFilterBytes / 4 - 1)), 1u << (i & 31)) >> (i & 31) & 1u;
-                    if (REST && i >= v0 && i < v1) atomicOr(mark_word(i, shift), 1u << (((i + shift) / E & 3) * 8 + (i + shift) % E));
                 }
             };
 #pragma unroll
@@ -863,7 +882,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                 const double l = row_loss<REST>(t, te.q_rest, p.k, p.c, s_q, s_lq, s_idx, s_s, s_first, lane);
                 if (lane == 0) {
                     p.loss[row] = te.any ? static_cast<float>(l) : 0.f;
-                    if (MODE == kDsLoss && p.saved != nullptr) *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) = make_float4(t.ref, t.Z, t.R, 0.f);
+                    if (MODE == kDsLoss && p.saved != nullptr) *reinterpret_cast<float4*>(p.saved + 4 * static_cast<size_t>(row)) = make_float4(t.m, t.Z, t.R, 0.f);
                 }
             }
             __syncwarp();
@@ -881,12 +900,19 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             const int* s_idx = reinterpret_cast<const int*>(s_q + 2 * p.k);
             const float* s_s = reinterpret_cast<const float*>(s_idx + p.k + 4);
             const uint8_t* s_first = reinterpret_cast<const uint8_t*>(s_s + p.k);
-            const uint8_t* mark = e0 + lay.mark;
             const Slice<T> sl = slice_of(row);
             // a warp that gives up says so to the others at the next meeting; all leave there
             bool ok = sb::wait(ent_full(eb), eph, abort);
             ok = sb::wait(row_full, n & 1u, abort) && ok;
             __syncwarp();
+            if (REST) {
+                // The listed columns take no part in the statistics (their gradient is written apart): each warp makes minus infinity of those in its own vectors.
+                for (int j = lane; j < p.k; j += 32) {
+                    const int i = s_idx[j], at = i - v0 + sl.shift;
+                    if (i >= v0 && i < v1 && (at / E / 32) % kDsWarps == warp) reinterpret_cast<T*>(ds_smem + lay.row)[at] = DsType<T>::round(-INFINITY);
+                }
+                __syncwarp();
+            }
             const uint4* buf = reinterpret_cast<const uint4*>(ds_smem + lay.row) + tid;
             const float ninf = -INFINITY;
             uint4 x[kDsVecs];
@@ -917,14 +943,6 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
                     if (j < sl.nv) {
                         float f[E];
                         DsType<T>::unpack(x[u], f);
-                        if (REST) {
-                            const uint32_t m = mark[j];
-                            if (m != 0) {
-#pragma unroll
-                                for (int e = 0; e < E; ++e)
-                                    if (m >> e & 1u) f[e] = -INFINITY;
-                            }
-                        }
 #pragma unroll
                         for (int e = 0; e < E; e += 2) {
                             float v, w;
@@ -960,8 +978,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
 
             // ---- what the row comes to, by every thread for itself
             const RowTeacher te = s_teacher[eb];
-            const float z = !REST ? 0.f : te.top == -INFINITY ? te.z : te.z * ex2((te.top - m) * p.c);
-            const RowTerms t = row_terms<REST>(m, R, z, te.q_sum, static_cast<float>(te.q_rest), static_cast<float>(te.mass));
+            const RowTerms t = row_terms<REST>(p.c, m, R, te.top, te.z, te.q_sum, static_cast<float>(te.q_rest), static_cast<float>(te.mass));
             if (tid == 0) {
                 s_terms[eb] = t;
                 sb::arrive(terms_full(eb));
@@ -1093,7 +1110,7 @@ static cudaError_t rows_launch(const DistillParams& p, int cluster, int clusters
 template <typename T, bool REST, int MODE>
 static int rows_try_as(const DistillParams& p, int cluster, cudaStream_t s) {
     if (p.slice / DsType<T>::E + 1 > kDsThreads * kDsVecs) return 1;
-    const RowsSmem<T> lay(p.slice, p.k, p.mark_bytes);
+    const RowsSmem<T> lay(p.slice, p.k);
     const int clusters = rows_resident<T, REST, MODE>(cluster, static_cast<size_t>(lay.total));
     if (clusters < 1 || p.M <= clusters) return 1;
     SLIM_CUDA_TRY((rows_launch<T, REST, MODE>(p, cluster, clusters, static_cast<size_t>(lay.total), s)));
