@@ -175,7 +175,8 @@ struct RowTerms {
     float ref, Z;            // the row's maximum (0 if that is minus infinity), the sum of all columns relative to it
     float m, R;
     float p_in;              // the set's mass
-    float inv_z, factor;     // of 2^((s - ref) c) in the gradient of the columns outside the set, but for the row's weight
+    float inv_z;
+    float out, factor;       // of 2^((s - out) c) in the gradient of the columns outside the set, but for the row's weight; out is m, or 0 for minus infinity
 };
 template <bool REST>
 __device__ __forceinline__ RowTerms row_terms(float c, float m, float R, float top, float z, float q_sum, float q_rest, float mass) {
@@ -184,18 +185,18 @@ __device__ __forceinline__ RowTerms row_terms(float c, float m, float R, float t
     t.ref = most == -INFINITY ? 0.f : most;
     t.m = m;
     t.R = R;
-    const float r = REST ? R * ex2((m - t.ref) * c) : R;
+    t.out = m == -INFINITY ? 0.f : m;
+    const float a = REST ? ex2((m - t.ref) * c) : 1.f, r = R * a;
     z = REST ? z * ex2((top - t.ref) * c) : 0.f;
     t.Z = r + z;
     const float over = rcp(t.Z);
     t.inv_z = t.Z == 0.f ? 0.f : over;
     t.p_in = z * t.inv_z;
-    t.factor = mass * t.inv_z;
-    // p (1 - q'/p') = 2^.. (p' - q') / (p' Z), where p' is what the set leaves of 1, or r / Z where that would cancel
-    if (REST && !(q_rest == 0.f)) {
-        const bool none = r < 1.17549435e-38f && t.Z == t.Z;        // below fp32's normal range there is nothing; a NaN in the set goes through
-        t.factor = t.Z == 0.f || none ? 0.f : t.p_in < 0.5f ? (q_sum - t.p_in) * rcp(1.f - t.p_in) * over : (r * over - q_rest) * rcp(r);
-    }
+    t.factor = mass * a * t.inv_z;
+    // p (1 - q'/p') = 2^.. (p' - q') / R, where p' is what the set leaves of 1, or r / Z where that would cancel.  R is at least 1, or 0 where there is nothing
+    // outside (a NaN in the set goes through): no factor exceeds 1, whatever p' is.
+    if (REST && !(q_rest == 0.f))
+        t.factor = R == 0.f && t.Z == t.Z ? 0.f : (t.p_in < 0.5f ? q_sum - t.p_in : r * over - q_rest) * rcp(R);
     return t;
 }
 // e^x in 64 bits for x up to a few (a log-probability), within 1e-14 of its value: x = n ln 2 + r after Cody and Waite (ln 2 = 355 / 512 and a
@@ -538,7 +539,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     T* r_grad = static_cast<T*>(p.grad) + static_cast<long long>(row) * p.ldg;
     T* g_base = r_grad + v0 - sl.shift;
     const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
-    const uint64_t neg2 = pair2(-t.ref, -t.ref), factor2 = pair2(factor, factor);
+    const uint64_t neg2 = pair2(-t.out, -t.out), factor2 = pair2(factor, factor);
     for (int j0 = 0; j0 < sl.nv; j0 += kDsVecs * kDsThreads) {
         if (MODE == kDsStep && sl.nv > kDsVecs * kDsThreads) {          // more than the registers hold: read again
 #pragma unroll
@@ -991,7 +992,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             if (MODE == kDsStep) {
                 T* g_base = r_grad + v0 - sl.shift;
                 const bool vectors = (reinterpret_cast<uintptr_t>(g_base) & 15u) == 0;
-                const uint64_t neg2 = pair2(-t.ref, -t.ref), factor2 = pair2(factor, factor);
+                const uint64_t neg2 = pair2(-t.out, -t.out), factor2 = pair2(factor, factor);
 #pragma unroll
                 for (int u = 0; u < kDsVecs; ++u) {
                     forget(x[u]);

@@ -109,6 +109,29 @@ def test_loss_where_the_student_leaves_the_rest_next_to_nothing(M, V, k, T, kind
     _check(*case, T, kind, loss1, None)
 
 
+@pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
+@pytest.mark.parametrize("T", [0.1, 0.25, 1.0])
+@pytest.mark.parametrize("M,V,k", SHAPES)
+def test_gradient_where_the_student_leaves_the_rest_next_to_nothing(M, V, k, T, kind):
+    case = _far(M, V, k, kind, T, V + 1)
+    _, grad, _, grad1 = _calls(*case, T)
+    _check(*case, T, kind, None, grad)
+    _check(*case, T, kind, None, grad1)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,V,k", SHAPES)
+def test_gradient_there_under_a_large_weight(M, V, k, kind):
+    """dloss / T of 1e6 (a loss scale; a low temperature): finite, as the definition's."""
+    T = 0.1
+    student, index, value, lse, dloss = _far(M, V, k, kind, T, V + 2)
+    case = (student, index, value, lse, dloss * 65536)
+    _, grad, _, grad1 = _calls(*case, T)
+    assert torch.isfinite(grad).all() and torch.isfinite(grad1).all()
+    _check(*case, T, kind, None, grad)
+    _check(*case, T, kind, None, grad1)
+
+
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
 @pytest.mark.parametrize("M,V,k", [(4, 700, 5), (2, 40001, 64), (400, 1001, 7)])
