@@ -448,7 +448,8 @@ int slim_fp8_linear(const void* x, int x_type, long long ldx, const void* codes,
  *   otherwise teacher_lse[t] = log sum_v exp(teacher logit_v / temperature) over the teacher's whole row:
  *     q_j = exp(value_j / temperature - teacher_lse), and all columns outside the entries are one more class with
  *     q' = max(0, 1 - sum_j q_j) and p' = 1 - sum of p over the entries' columns: loss[t] += q' (log q' - log p')
- *     (q' = 0 if there is no such column)
+ *     (q' = 0 if there is no such column, and where 1 - sum_j q_j is at most 2^-22 (1 + |teacher_lse|), up to a half: that is what rounding makes of a
+ *     log-sum-exp in fp32, and a vocabulary that teacher and student mask alike has p' = 0.  The values themselves are taken as exact.)
  *   grad[t][v] = dloss[t] * d loss[t] / d logits[t][v]
  * An entry whose index lies outside [0, V) is absent (padding: -1).  A row without a present entry, or (teacher_lse == NULL)
  * whose present values are all minus infinity, has loss 0 and gradient 0, whatever its logits.  An index that occurs

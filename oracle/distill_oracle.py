@@ -45,7 +45,9 @@ def distill(logits, index, value, temperature, lse=None, dloss=None):
                 p_rest = p[outside].sum()
                 top_out = s[t][outside].max(initial=-np.inf)
                 e_out = np.where(outside, np.exp(s[t] - top_out), 0.0) if top_out > -np.inf else np.zeros(V)
-                q_rest = max(0.0, 1.0 - mass) if outside.any() else 0.0
+                q_rest = 1.0 - mass if outside.any() else 0.0
+                if q_rest <= min(2.0 ** -22 * (1.0 + abs(float(lse[t]))), 0.5):       # what an fp32 log-sum-exp is off by
+                    q_rest = 0.0
                 factor += q_rest
                 if q_rest > 0:
                     lp_rest = (top_out - top) + np.log(e_out.sum()) - np.log(Z) if top_out > -np.inf else -np.inf

@@ -215,6 +215,13 @@ __device__ __forceinline__ double exp_log(double x) {
     const double y = fma(fma(ef, r4, cd), r4, ab);
     return __hiloint2double(__double2hiint(y) + (static_cast<int>(n) << 20), __double2loint(y));
 }
+// What the entries leave of the teacher's mass.  Its log-sum-exp is fp32 and moves log q by its error: 2^-24 of the largest logit / T from the division, of the
+// result from the last addition, and a few 2^-24 from the sum and its logarithm.  What is within twice that (2^-22 (1 + |lse|)) is that error and counts as
+// nothing; it would otherwise be weighed against a p' that may be 0.  NaN stays NaN.
+__device__ __forceinline__ double rest_mass(double q_sum, float lse) {
+    const double rest = 1.0 - q_sum;
+    return rest <= static_cast<double>(fminf(0x1p-22f * (1.f + fabsf(lse)), 0.5f)) ? 0.0 : rest;
+}
 __device__ __forceinline__ float redux_max(float v) {
     float r;
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
@@ -514,7 +521,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
         columns = static_cast<int>(__reduce_add_sync(0xffffffffu, columns));
-        if (columns < p.V) q_rest = q_sum >= 1.0 ? 0.0 : 1.0 - q_sum;         // NaN stays NaN
+        if (columns < p.V) q_rest = rest_mass(q_sum, lse);
     }
     const double mass = q_sum + q_rest;
     const RowTerms t = row_terms<REST>(p.c, m, static_cast<float>(R), top, z, static_cast<float>(q_sum), static_cast<float>(q_rest), static_cast<float>(mass));
@@ -823,7 +830,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             }
             if (lane == 0) {
                 RowTeacher t;
-                t.q_rest = REST && columns < p.V ? (q_sum >= 1.0 ? 0.0 : 1.0 - q_sum) : 0.0;       // NaN stays NaN
+                t.q_rest = REST && columns < p.V ? rest_mass(q_sum, lse) : 0.0;
                 t.mass = q_sum + t.q_rest;
                 t.d = static_cast<double>(weight) * p.inv_t;
                 t.q_sum = static_cast<float>(q_sum);

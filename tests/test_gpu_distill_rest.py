@@ -182,3 +182,54 @@ def test_losses_that_are_not_finite_are_the_definitions(M, rest):
         assert np.isfinite(got[~odd]).all()
         if grad is not None:
             np.testing.assert_array_equal(np.isnan(grad.cpu().numpy()), np.isnan(want_grad))
+
+
+def _masked(M, V, k, T, mask, seed):
+    """A vocabulary of which all but the k entries are masked, teacher and student alike; the teacher's log-sum-exp as torch takes it, in fp32."""
+    g = torch.Generator().manual_seed(seed)
+    index = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(M)])
+    value = torch.randn(M, k, generator=g) * 5 + 40 * torch.randn(M, 1, generator=g)
+    teacher = torch.full((M, V), mask).scatter_(1, index, value)
+    student = torch.full((M, V), mask).scatter_(1, index, value + torch.randn(M, k, generator=g))
+    return student, index, value, torch.logsumexp(teacher / T, 1), torch.rand(M, generator=g) + 0.5
+
+
+@pytest.mark.parametrize("mask", [-float("inf"), torch.finfo(torch.float32).min, -1e4])
+@pytest.mark.parametrize("T", [0.5, 1.0, 3.0])
+@pytest.mark.parametrize("M,V,k", [(250, 700, 8), (1000, 1001, 40), (60, 40001, 3)])
+def test_a_vocabulary_masked_outside_the_entries(M, V, k, T, mask):
+    """All of the teacher's mass is listed: what 1 - sum q is off by is the rounding of its log-sum-exp, and counts as nothing.  So the loss is the KL over
+    the entries, in 64 bits here, and outside nothing has a gradient.  A log-sum-exp that is off by at most 2^-22 (1 + |lse|) shifts log q by that much."""
+    student, index, value, lse, dloss = _masked(M, V, k, T, mask, V + k)
+    lq, s = value.double() / T - lse.double()[:, None], torch.gather(student, 1, index).double() / T
+    lp = torch.log_softmax(s, 1)
+    q = torch.exp(lq)
+    assert (1.0 - q.sum(1) > 0).sum() > M // 5       # the case is there
+    want = (q * (lq - lp)).sum(1)
+    # log p's error, as in _check: distances of at most some 60 units / T, a chain of few terms of note
+    D = (s.max(1, keepdim=True).values - s)
+    u = 2.0 ** -24
+    tol = (q * (D * 3 * u)).sum(1) + (33 * 2 + 49 + 30) * u + (torch.exp(lp) * D).sum(1) * 3 * u + u * want.abs()
+    loss, grad, loss1, grad1 = _calls(student, index, value, lse, dloss, T)
+    for l, gr in ((loss, grad), (loss1, grad1)):
+        err = (l.cpu().double() - want).abs()
+        assert (err <= tol).all(), (err / tol).max()
+        assert (gr.cpu().scatter(1, index, 0.0) == 0).all()
+        inside = (torch.exp(lp) * q.sum(1, keepdim=True) - q) * dloss.double()[:, None] / T
+        err = (torch.gather(gr.cpu(), 1, index).double() - inside).abs()
+        bound = (torch.exp(lp) * (D.clamp(max=150) * 3 * u + tol[:, None] + 150 * u) + 1e-12) * dloss.double()[:, None] / T + u * inside.abs() + 2.0 ** -120
+        assert (err <= bound).all(), (err / bound).max()
+
+
+@pytest.mark.parametrize("M", [6, 400])
+def test_a_rest_above_the_rounding_of_the_log_sum_exp_counts(M):
+    """Just more than 2^-22 (1 + |lse|) outside the entries: the definition's loss, with all of it."""
+    student, index, value, lse, dloss = _far(M, 1000, 8, "fp32", 1.0, 3)
+    value += 30.0 * torch.randn(M, 1, generator=torch.Generator().manual_seed(1))
+    exact = torch.logsumexp(value.double(), 1)
+    lse = (exact + 2.0 ** -20 * (1 + exact.abs())).float()
+    rest = 1 - torch.exp(value.double() - lse.double()[:, None]).sum(1)
+    assert (rest > 2.0 ** -22 * (1 + lse.double().abs())).all() and (rest < 1e-3).all()
+    loss, grad, loss1, grad1 = _calls(student, index, value, lse, dloss, 1.0)
+    _check(student, index, value, lse, dloss, 1.0, "fp32", loss, grad)
+    _check(student, index, value, lse, dloss, 1.0, "fp32", loss1, grad1)

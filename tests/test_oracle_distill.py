@@ -54,3 +54,20 @@ def test_gradient_against_differences(rest, dup, T):
         np.testing.assert_allclose(grad[:, v], num, atol=1e-9)
     assert (grad[2] == 0).all()
     np.testing.assert_allclose(grad.sum(1), 0, atol=1e-12)
+
+
+def test_a_log_sum_exp_in_fp32_makes_no_rest():
+    """All of the teacher's mass listed: what its rounded log-sum-exp leaves or adds is no class of its own, also where the student has nothing there."""
+    student, teacher, index, value = _case(200, 40, 6, seed=4)
+    rows = np.arange(200)[:, None]
+    masked_teacher, masked_student = np.full_like(teacher, -np.inf), np.full_like(student, -np.inf)
+    masked_teacher[rows, index], masked_student[rows, index] = value, student[rows, index]
+    lse = np.log(np.exp(masked_teacher).sum(1)).astype(np.float32)
+    assert (np.exp(value - lse[:, None].astype(np.float64)).sum(1) < 1).sum() > 50
+    loss, grad, parts = distill(masked_student, index, value, 1.0, lse)
+    want, _, _ = distill(student[rows, index], np.tile(np.arange(6), (200, 1)), value, 1.0)
+    np.testing.assert_allclose(loss, want, atol=1e-5)
+    assert (parts["q_rest"] == 0).all() and np.isfinite(grad).all()
+    # and a little more than that is one
+    loss, _, parts = distill(student, index, value, 1.0, np.log(np.exp(value).sum(1)) + 1e-5)
+    np.testing.assert_allclose(parts["q_rest"], 1e-5, rtol=1e-2)
