@@ -428,8 +428,9 @@ int slim_fp8_workspace_bytes(int M, int N, int K, size_t* out_bytes);
 /* y[m][n] = sum_g sx[m][g] * scales[n/128][g] * sum_{k in block g} e4m3(x)[m][k] * codes[n][k], by the tensor
  * cores (fp32 accumulator; the scales are applied inside); one rounding to y.  Any M >= 1 (one token and thousands alike) and N; K a multiple of 16.
  *   x fp16 or bf16 [M][K], row stride ldx (a multiple of 8 elements); y of x's type or fp32 [M][N], row stride ldy.
- * scales: powers of two from 2^-126 to 2^127, as the quantizer gives them (the tensor cores take their exponents; of any other value
- * only the exponent counts).  NaN or infinity in x gives NaN in that token's row of y alone, NaN codes (0x7f, 0xff) in the outputs of their rows of W.
+ * scales: powers of two from 2^-126 to 2^127, as the quantizer gives them: the tensor cores take exponents.  Any other value (a checkpoint's arbitrary
+ * fp32 scale, zero, a negative one) makes NaN of the outputs of its 128 rows of W; such a layer is dequantised and quantised again by slim_fp8_quantize.
+ * NaN or infinity in x gives NaN in that token's row of y alone, NaN codes (0x7f, 0xff) in the outputs of their rows of W.
  * The gradient of x for a frozen W, dx = dy * W, is the same call on the transposed layer: codes^T [K][N] and scales^T, with x = dy.
  * Deterministic.  A wait that gives up is reported by slim_workspace_status. */
 #define SLIM_FP8_MAX_K 262144

@@ -416,7 +416,8 @@ def fp8_workspace_bytes(M: int, N: int, K: int) -> int:
 def fp8_linear(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor | None = None,
                out_dtype: torch.dtype | None = None) -> torch.Tensor:
     """y = x W^T with W in e4m3 under a scale per block of 128 x 128, x (fp16 or bf16 [M][K], rows may be strided) quantised
-    inside the call (slim_fp8_linear).  y is of x's type, or fp32 (out_dtype, or out's)."""
+    inside the call (slim_fp8_linear).  y is of x's type, or fp32 (out_dtype, or out's).  Scales that are not powers of two make NaN of their
+    rows' outputs; Fp8Linear refuses them."""
     y = (_host or host()).fp8_linear(_entry["slim_fp8_linear"], x, codes, scales, workspace, out, -1 if out_dtype is None else _TYPES.get(out_dtype, 3))
     if y is not None:
         if type(y) is int:

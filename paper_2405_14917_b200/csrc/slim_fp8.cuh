@@ -22,8 +22,14 @@ __device__ __forceinline__ uint32_t scale_bits(uint32_t amax) {
     const int e = static_cast<int>(amax >> 23) - 8 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
     return static_cast<uint32_t>(max(e, 1)) << 23;
 }
-// 1 / s for s of scale_bits (2^-126 .. 2^119): exact.
+// 1 / s for s of scale_bits (2^-126 .. 2^120): exact.
 __device__ __forceinline__ float inverse_scale(uint32_t bits) { return __uint_as_float((254u << 23) - bits); }
+
+// E8M0 of a scale of W: its exponent if it is a power of two from 2^-126 to 2^127, else 255, NaN, so that no other scale passes for the power of two below it.
+__device__ __forceinline__ uint32_t e8m0(uint32_t bits) {
+    const uint32_t e = bits >> 23;                 // 256 and more with a sign
+    return (bits & 0x7fffffu) == 0 && e - 1u < 254u ? e : 255u;
+}
 
 // Four codes of v * inv.  NaN gives NaN (0x7f or 0xff); `checked` makes NaN of infinities too (e4m3 has none, and 448 would pass for a value).
 template <bool checked>

@@ -188,7 +188,7 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
                 w_now = w_next;
                 w_next = i + 32 + lane < steps ? __float_as_uint(__ldg(sw + i + 32 + lane)) : 0u;
             }
-            const uint32_t w = __shfl_sync(0xffffffffu, w_now, i & 31) >> 23 & 0xffu;
+            const uint32_t w = f8::e8m0(__shfl_sync(0xffffffffu, w_now, i & 31));
             uint32_t v[8] = {w, w, w, w, 0, 0, 0, 0};
             if (C::TAKES_X) {
                 if (!tc::warp_wait(x_full(s), ph, abort)) break;

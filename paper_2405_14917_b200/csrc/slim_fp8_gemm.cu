@@ -214,7 +214,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap x_map, const __grid_constant
             };
             auto put = [&](const Words& v) {
                 const int b = issued & 1;
-                uint32_t own = (v.w >> 23 & 0xffu) << (8 * (lane & 3)), ww[8];
+                uint32_t own = f8::e8m0(v.w) << (8 * (lane & 3)), ww[8];
                 own |= __shfl_xor_sync(0xffffffffu, own, 1);
                 own |= __shfl_xor_sync(0xffffffffu, own, 2);
 #pragma unroll
