@@ -13,6 +13,7 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import os
+import threading
 import warnings
 
 import numpy as np
@@ -703,6 +704,9 @@ class QuantLinear:
         return self.packed.numel() + 2 * 2 * G * self.N + G + 2 * M * self.K + 2 * M * self.N
 
 
+_layout = threading.Lock()
+
+
 class Fp8Linear:
     """One layer in 8-bit floats resident on the device: e4m3 codes [N][K] and a scale per block of 128 x 128.
 
@@ -718,7 +722,7 @@ class Fp8Linear:
             raise ValueError("codes must be [N][K] and scales [ceil(N/128)][ceil(K/128)]")
         self.codes, self.scales = codes, scales
         self.N, self.K = codes.shape
-        self._codes_t = self._scales_t = None
+        self._transposed = None                        # codes and scales for input_grad, complete on the device once they are here
 
     @classmethod
     def from_weight(cls, W: torch.Tensor) -> "Fp8Linear":
@@ -736,15 +740,25 @@ class Fp8Linear:
         return fp8_linear(x, self.codes, self.scales, workspace, out, out_dtype)
 
     def prepare_input_grad(self) -> None:
-        """Lays the transposed codes and scales out, unless they are there already."""
-        if self._codes_t is None:
-            if self.N % 16:
-                raise ValueError("the gradient of the input needs a number of output features that is a multiple of 16")
-            self._codes_t = self.codes.view(torch.uint8).t().contiguous().view(torch.float8_e4m3fn)
-            self._scales_t = self.scales.t().contiguous()
+        """Lays the transposed codes and scales out, unless they are there already, and waits for them: they may then be read on any stream.
+        Not under capture, which would only record it."""
+        if self._transposed is not None:
+            return
+        if self.N % 16:
+            raise ValueError("the gradient of the input needs a number of output features that is a multiple of 16")
+        with _layout, _device_of(self.codes):
+            if self._transposed is not None:
+                return
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("prepare_input_grad() has to be called before the stream is captured")
+            codes_t = self.codes.view(torch.uint8).t().contiguous().view(torch.float8_e4m3fn)
+            scales_t = self.scales.t().contiguous()
+            torch.cuda.current_stream().synchronize()
+            self._transposed = codes_t, scales_t
 
     def input_grad(self, dy: torch.Tensor, workspace: torch.Tensor, out: torch.Tensor | None = None,
                    out_dtype: torch.dtype | None = None) -> torch.Tensor:
-        """dx = dy W for dy [M][N], quantised in the call like forward's x."""
-        self.prepare_input_grad()
-        return fp8_linear(dy, self._codes_t, self._scales_t, workspace, out, out_dtype)
+        """dx = dy W for dy [M][N], quantised in the call like forward's x.  The first call prepares, where that has not been done."""
+        if self._transposed is None:
+            self.prepare_input_grad()
+        return fp8_linear(dy, *self._transposed, workspace, out, out_dtype)
