@@ -427,7 +427,8 @@ int slim_fp8_workspace_bytes(int M, int N, int K, size_t* out_bytes);
 
 /* y[m][n] = sum_g sx[m][g] * scales[n/128][g] * sum_{k in block g} e4m3(x)[m][k] * codes[n][k], by the tensor
  * cores (fp32 accumulator; the scales are applied inside); one rounding to y.  Any M >= 1 (one token and thousands alike) and N; K a multiple of 16.
- *   x fp16 or bf16 [M][K], row stride ldx (a multiple of 8 elements); y of x's type or fp32 [M][N], row stride ldy.
+ *   x fp16 or bf16 [M][K], row stride ldx (a multiple of 8 elements); y of x's type or fp32 [M][N], row stride ldy, 16-byte aligned.
+ * y may lie over x beyond 16 tokens (x has been quantised before y is written); up to 16, a y that shares memory with x is refused.
  * scales: powers of two from 2^-126 to 2^127, as the quantizer gives them: the tensor cores take exponents.  Any other value (a checkpoint's arbitrary
  * fp32 scale, zero, a negative one) makes NaN of the outputs of its 128 rows of W; such a layer is dequantised and quantised again by slim_fp8_quantize.
  * NaN or infinity in x gives NaN in that token's row of y alone, NaN codes (0x7f, 0xff) in the outputs of their rows of W.
@@ -460,7 +461,8 @@ int slim_fp8_linear(const void* x, int x_type, long long ldx, const void* codes,
  *   logits  [M][V], row stride ld >= V elements, of SLIM_F32, SLIM_F16 or SLIM_BF16 (aligned to an element)
  *   index   int32 or int64 (index_bytes 4 or 8) [M][k]; value [M][k] of any of the three types; teacher_lse, dloss, loss fp32 [M]
  *   saved   fp32 [M][4], 16-byte aligned: what _grad needs of _loss (same logits, entries, teacher_lse and temperature); may be NULL in _loss
- *   grad    [M][V] of the logits' type, row stride ldg >= V; may be the logits themselves (same pointer and stride)
+ *   grad    [M][V] of the logits' type, row stride ldg >= V; may be the logits themselves (same pointer and stride); one that shares memory with them otherwise
+ *           is refused.  No output may lie over another argument.
  * _step is _loss and _grad in one call: rows up to 65000 columns (half as many of fp32) are read once, longer ones a second
  * time, from L2 as a rule.  Sums over the columns in fp32, what is computed per entry in fp64; deterministic.
  * 1 <= k <= SLIM_DISTILL_MAX_K, V <= SLIM_DISTILL_MAX_V, temperature > 0.  A device-side wait of the many-rows kernels that gives up leaves NaN

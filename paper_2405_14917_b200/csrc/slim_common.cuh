@@ -41,6 +41,24 @@ __device__ __forceinline__ void report_timeout(void* header, bool uses_flags) {
     if (uses_flags) atomicOr(static_cast<unsigned int*>(header) + 1, 1u);
 }
 
+// Do two matrices of M rows (row strides and lengths in bytes, stride >= length) share a byte?  With equal strides row n of b starts d bytes behind the start of
+// row n + q of a; with others row by row, where the two lie in each other's range at all.
+inline bool rows_share(const void* pa, long long lda, long long wa, const void* pb, long long ldb, long long wb, int M) {
+    const long long diff = static_cast<long long>(reinterpret_cast<uintptr_t>(pb) - reinterpret_cast<uintptr_t>(pa));
+    if (M < 1 || wa < 1 || wb < 1 || diff >= (M - 1) * lda + wa || -diff >= (M - 1) * ldb + wb) return false;
+    if (M == 1) return true;
+    auto floor_div = [](long long x, long long y) { return x / y - (x % y < 0 ? 1 : 0); };
+    if (lda == ldb) {
+        const long long q = floor_div(diff, lda), d = diff - q * lda;
+        return (d < wa && q < M && q > -M) || (d + wb > lda && q + 1 < M && q + 1 > -M);
+    }
+    for (long long m = 0; m < M; ++m) {                // rows of b that begin before the end of a's row m and end behind its start
+        const long long first = floor_div(m * lda - wb - diff, ldb) + 1, last = floor_div(m * lda + wa - 1 - diff, ldb);
+        if (first <= last && first < M && last >= 0) return true;
+    }
+    return false;
+}
+
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Scratch bytes slim_mpq_gemm wants for (M, N) on the current device (256 when it needs none).

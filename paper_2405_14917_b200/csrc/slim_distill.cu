@@ -1168,6 +1168,9 @@ static int distill(int mode, const void* logits, int type, long long ld, const v
     if (!aligned_to(logits, es) || !aligned_to(grad, es) || !aligned_to(index, index_bytes) || !aligned_to(value, value_type == SLIM_F32 ? 4 : 2) ||
         !aligned_to(lse, 4) || !aligned_to(dloss, 4) || !aligned_to(loss, 4) || !aligned16(saved))
         return SLIM_ERR_ALIGNMENT;
+    if (mode != kDsLoss && !(grad == logits && (ldg == ld || M == 1)) &&
+        rows_share(logits, ld * es, static_cast<long long>(V) * es, grad, ldg * es, static_cast<long long>(V) * es, M))
+        return SLIM_ERR_INVALID_ARG;
     const int E = 16 / es, held = kDsThreads * kDsVecs;            // vectors that a CTA's registers hold
     DistillParams p;
     memset(&p, 0, sizeof p);

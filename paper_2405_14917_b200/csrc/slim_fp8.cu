@@ -206,6 +206,8 @@ extern "C" int slim_fp8_linear(const void* x, int x_type, long long ldx, const v
     slim_fp8_workspace_bytes(M, N, K, &need);
     if (workspace == nullptr || workspace_bytes < need) return SLIM_ERR_WORKSPACE;
     if (!slim::aligned16(workspace)) return SLIM_ERR_ALIGNMENT;
+    const long long ys = y_type == SLIM_F32 ? 4 : 2;
+    if (slim::fp8_few_takes_x(M) && slim::rows_share(x, 2 * ldx, 2ll * K, y, ys * ldy, ys * N, M)) return SLIM_ERR_INVALID_ARG;
     slim::Fp8Args a;
     memset(&a, 0, sizeof a);
     a.x = x; a.x_type = x_type; a.ldx = ldx;
