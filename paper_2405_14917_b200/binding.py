@@ -366,6 +366,8 @@ def _rows(t: torch.Tensor, name: str, dtypes, device=None) -> int:
     if device is not None and t.device != device:
         raise ValueError(f"{name}: on {t.device}, expected {device}")
     rows, cols = t.shape
+    if max(rows, cols) > 2 ** 31 - 1:
+        raise ValueError(f"{name}: more rows or columns than the library counts")
     if cols > 1 and t.stride(1) != 1 or rows > 1 and t.stride(0) < cols:
         raise ValueError(f"{name}: rows must be contiguous and must not overlap")
     return t.stride(0) if rows > 1 else max(cols, 1)
