@@ -16,6 +16,7 @@
 // computed of the entries, and the loss, is fp64, because a small loss is the difference of large terms.
 // Measured: loss of 512 x 152064 bf16 45 us, its gradient 57 (5.5 TB/s), both in one call 88; 777 x 50257 fp32 in one call 74, 4096 x 32000 bf16 131;
 // loss of 16 x 32000 8.2, all of it latency.
+#include "slim_exp.cuh"
 #include "slim_gemv_i8.cuh"
 
 #include <cuda_bf16.h>
@@ -198,22 +199,6 @@ __device__ __forceinline__ RowTerms row_terms(float c, float m, float R, float t
     if (REST && !(q_rest == 0.f))
         t.factor = R == 0.f && t.Z == t.Z ? 0.f : (t.p_in < 0.5f ? q_sum - t.p_in : r * over - q_rest) * rcp(R);
     return t;
-}
-// e^x in 64 bits for x up to a few (a log-probability), within 1e-14 of its value: x = n ln 2 + r after Cody and Waite (ln 2 = 355 / 512 and a
-// rest, so that n times the first is exact), Taylor's series of e^r to the eleventh power (|r| < 0.35: 0.35^12 / 12! < 1e-14) summed in pairs,
-// times 2^n.  Half as many dependent steps as a general exp(), which takes what lies beyond.
-__device__ __forceinline__ double exp_log(double x) {
-    if (x > 80.0) return exp(x);
-    if (x < -700.0) return 0.0;
-    const double n = rint(x * 1.44269504088896340736);
-    double r = fma(n, -355.0 / 512, x);
-    r = fma(n, 2.12194440054690582768e-4, r);
-    const double r2 = r * r, r4 = r2 * r2;
-    const double a = fma(r, 1.0, 1.0), b = fma(r, 1.0 / 6, 1.0 / 2), c = fma(r, 1.0 / 120, 1.0 / 24), d = fma(r, 1.0 / 5040, 1.0 / 720),
-                 e = fma(r, 1.0 / 362880, 1.0 / 40320), f = fma(r, 1.0 / 39916800, 1.0 / 3628800);
-    const double ab = fma(b, r2, a), cd = fma(d, r2, c), ef = fma(f, r2, e);
-    const double y = fma(fma(ef, r4, cd), r4, ab);
-    return __hiloint2double(__double2hiint(y) + (static_cast<int>(n) << 20), __double2loint(y));
 }
 // What the entries leave of the teacher's mass.  Its log-sum-exp is fp32 and moves log q by its error: 2^-24 of the largest logit / T from the division, of the
 // result from the last addition, and a few 2^-24 from the sum and its logarithm.  What is within twice that (2^-22 (1 + |lse|)) is that error and counts as
