@@ -317,6 +317,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     uint8_t* s_first = reinterpret_cast<uint8_t*>(s_s + p.k);          // [k] no entry before it has this column
     uint32_t* s_mark = reinterpret_cast<uint32_t*>(ds_smem + entry_bytes(p.k));    // REST: bit e of byte j: element e of vector j is listed
     __shared__ float2 s_part[kDsWarps];                                // maximum and sum of every warp's columns
+    __shared__ float4 s_set[kDsWarps];                                 // REST: of every warp's entries the largest logit, the sum of exponentials relative to it, the columns
     __shared__ float2 s_slice;                                         // maximum and sum of this slice, for the cluster
     __shared__ double s_row[2];                                         // the teacher's listed mass; whether there is any
 
@@ -404,6 +405,24 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     }
     twice = __syncthreads_or(twice);
 
+    // A warp's entries' part of the set's columns: every column once, by its first entry.
+    auto set_part = [&] {
+        float top = -INFINITY, z = 0.f;
+        int columns = 0;
+        if (tid < p.k && s_first[tid]) { top = early; ++columns; }
+        for (int j = tid + kDsThreads; j < p.k; j += kDsThreads)
+            if (s_first[j]) { top = fmaxf(top, s_s[j]); ++columns; }
+        top = redux_max(top);
+        const float ref = top == -INFINITY ? 0.f : top;
+        if (tid < p.k && s_first[tid]) z = ex2((early - ref) * p.c);
+        for (int j = tid + kDsThreads; j < p.k; j += kDsThreads)
+            if (s_first[j]) z += ex2((s_s[j] - ref) * p.c);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        columns = static_cast<int>(__reduce_add_sync(0xffffffffu, columns));
+        if (lane == 0) s_set[warp] = make_float4(top, z, __int_as_float(columns), 0.f);
+    };
+
     // ---- the row's maximum and sum of exponentials, of the columns outside the set with REST
     float m;
     double R;                                        // sum over the columns (outside the set) of 2^((s - m) c)
@@ -468,6 +487,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
         for (int o = 16; o > 0; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
         if (lane == 0) s_part[warp] = make_float2(wm, ws);
         if (tid < p.k) s_s[tid] = early;
+        if (REST) set_part();
         __syncthreads();
         auto join = [&](float2 part, bool in) {
             m = in ? part.x : -INFINITY;
@@ -486,6 +506,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
         m = sv.x;
         R = REST ? sv.z : sv.y;
         if (tid < p.k) s_s[tid] = early;
+        if (REST) set_part();
         __syncthreads();
         if (ranks > 1) cluster_sync_all();           // grad may be logits: every CTA of the row has its entries' logits
     }
@@ -496,16 +517,13 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
     double q_rest = 0.0;
     float z = 0.f, top = -INFINITY;
     if (REST) {
-        int columns = 0;
-        for (int j = lane; j < p.k; j += 32)
-            if (s_first[j]) { top = fmaxf(top, s_s[j]); ++columns; }
-        top = redux_max(top);
-        const float ref = top == -INFINITY ? 0.f : top;
-        for (int j = lane; j < p.k; j += 32)
-            if (s_first[j]) z += ex2((s_s[j] - ref) * p.c);
+        // the warps' parts of the set
+        const float4 part = s_set[lane % kDsWarps];
+        top = redux_max(part.x);
+        z = part.x == -INFINITY ? part.y : part.y * ex2((part.x - top) * p.c);
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        columns = static_cast<int>(__reduce_add_sync(0xffffffffu, columns));
+        for (int o = kDsWarps / 2; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        const int columns = static_cast<int>(__reduce_add_sync(0xffffffffu, lane < kDsWarps ? __float_as_int(part.z) : 0));
         if (columns < p.V) q_rest = rest_mass(q_sum, lse);
     }
     const double mass = q_sum + q_rest;
