@@ -175,7 +175,6 @@ __device__ __forceinline__ float rcp(float v) {      // within an ulp
 struct RowTerms {
     float ref, Z;            // the row's maximum (0 if that is minus infinity), the sum of all columns relative to it
     float m, R;
-    float p_in;              // the set's mass
     float inv_z;
     float out, factor;       // of 2^((s - out) c) in the gradient of the columns outside the set, but for the row's weight; out is m, or 0 for minus infinity
 };
@@ -187,17 +186,23 @@ __device__ __forceinline__ RowTerms row_terms(float c, float m, float R, float t
     t.m = m;
     t.R = R;
     t.out = m == -INFINITY ? 0.f : m;
-    const float a = REST ? ex2((m - t.ref) * c) : 1.f, r = R * a;
-    z = REST ? z * ex2((top - t.ref) * c) : 0.f;
+    float a = 1.f, r = R;                              // of the two parts the one with the smaller maximum is brought to the other's
+    if (REST) {
+        const float d = ex2((fminf(m, top) - t.ref) * c);
+        const bool set_leads = top > m;
+        a = set_leads ? d : 1.f;
+        r = R * a;
+        z *= set_leads ? 1.f : d;
+    } else z = 0.f;
     t.Z = r + z;
     const float over = rcp(t.Z);
     t.inv_z = t.Z == 0.f ? 0.f : over;
-    t.p_in = z * t.inv_z;
+    const float p_in = z * t.inv_z;                  // the set's mass
     t.factor = mass * a * t.inv_z;
     // p (1 - q'/p') = 2^.. (p' - q') / R, where p' is what the set leaves of 1, or r / Z where that would cancel.  R is at least 1, or 0 where there is nothing
     // outside (a NaN in the set goes through): no factor exceeds 1, whatever p' is.
     if (REST && !(q_rest == 0.f))
-        t.factor = R == 0.f && t.Z == t.Z ? 0.f : (t.p_in < 0.5f ? q_sum - t.p_in : r * over - q_rest) * rcp(R);
+        t.factor = R == 0.f && t.Z == t.Z ? 0.f : (p_in < 0.5f ? q_sum - p_in : r * over - q_rest) * rcp(R);
     return t;
 }
 // What the entries leave of the teacher's mass.  Its log-sum-exp is fp32 and moves log q by its error: 2^-24 of the largest logit / T from the division, of the
@@ -350,6 +355,7 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
         s_lq[tid] = static_cast<double>(teacher_logit(p, own_value)) * p.inv_t;
         if (i >= 0) early = DsType<T>::one(r_logits[i]);
     }
+#pragma unroll 1
     for (int j = tid + kDsThreads; j < p.k; j += kDsThreads) {
         const int i = column_of(p, raw_index(p, entry0 + j));
         s_idx[j] = i;
@@ -410,11 +416,13 @@ __global__ void __launch_bounds__(kDsThreads, 2) distill_kernel(const DistillPar
         float top = -INFINITY, z = 0.f;
         int columns = 0;
         if (tid < p.k && s_first[tid]) { top = early; ++columns; }
+#pragma unroll 1
         for (int j = tid + kDsThreads; j < p.k; j += kDsThreads)
             if (s_first[j]) { top = fmaxf(top, s_s[j]); ++columns; }
         top = redux_max(top);
         const float ref = top == -INFINITY ? 0.f : top;
         if (tid < p.k && s_first[tid]) z = ex2((early - ref) * p.c);
+#pragma unroll 1
         for (int j = tid + kDsThreads; j < p.k; j += kDsThreads)
             if (s_first[j]) z += ex2((s_s[j] - ref) * p.c);
 #pragma unroll
@@ -918,6 +926,7 @@ __global__ void __launch_bounds__(kDsRowsThreads, 2) distill_rows_kernel(const D
             __syncwarp();
             if (REST) {
                 // The listed columns take no part in the statistics (their gradient is written apart): each warp makes minus infinity of those in its own vectors.
+#pragma unroll 1
                 for (int j = lane; j < p.k; j += 32) {
                     const int i = s_idx[j], at = i - v0 + sl.shift;
                     if (i >= v0 && i < v1 && (at / E / 32) % kDsWarps == warp) reinterpret_cast<T*>(ds_smem + lay.row)[at] = DsType<T>::round(-INFINITY);
@@ -1192,11 +1201,13 @@ static int distill(int mode, const void* logits, int type, long long ld, const v
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int vecs = V / E + 2;
     // Many rows that one CTA's registers hold, or for the step two CTAs': the kernel that takes row after row.  (us, that one / a CTA per
-    // row: step of 4096 x 32000 bf16 131 / 173, of 2000 x 40000 by two 99 / 122; loss of 4096 x 32000 71 / 106, of 4096 x 8000 49 / 91.  By three and more the CTAs of
-    // a row wait for each other longer than the second reading, from L2, takes: 1024 x 65536 125 / 78, 512 x 152064 121 / 93, 777 x 50257 fp32 106 / 84.)
+    // row, with the rest: step of 4096 x 32000 bf16 125 / 178, of 2000 x 40000 by two 99 / 140; loss of 4096 x 32000 70 / 117, of 4096 x 8000 51 / 103.  By three and
+    // more the CTAs of a row wait for each other longer than the second reading, from L2, takes: 1024 x 65536 128 / 81, 512 x 152064 121 / 89, 777 x 50257 fp32 95 / 74.)
+    // Both CTAs of a pair prepare all entries, which is what the row waits for when there are many: 2000 x 32000 fp32 with 128, 200 and 310 113 / 132, 149 / 145, 196 / 165,
+    // 2000 x 60000 bf16 with 256 and 310 170 / 183, 200 / 196.
     if (mode != kDsGrad && vecs <= (mode == kDsStep ? 2 : 1) * (held - 1)) {
         cut(vecs <= held - 1 ? 1 : 2);
-        const int taken = mode == kDsStep ? rows_try<kDsStep>(p, type, p.ranks, s) : rows_try<kDsLoss>(p, type, p.ranks, s);
+        const int taken = p.ranks > 1 && k > 40 * E ? 1 : mode == kDsStep ? rows_try<kDsStep>(p, type, p.ranks, s) : rows_try<kDsLoss>(p, type, p.ranks, s);
         if (taken <= 0) return taken;
     }
     // Otherwise the cluster that ends soonest: a CTA has its part of a row to read, and what a row costs besides takes as long as some 6500 vectors.

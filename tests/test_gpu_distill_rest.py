@@ -132,6 +132,16 @@ def test_gradient_there_under_a_large_weight(M, V, k, kind):
     _check(*case, T, kind, None, grad1)
 
 
+@pytest.mark.parametrize("M,V,k,kind", [(200, 32000, 160, "fp32"), (200, 32000, 161, "fp32"), (200, 60000, 300, "bf16"), (160, 65001, 321, "fp16"),
+                                        (300, 30001, 330, "bf16"), (320, 4001, 770, "fp32")])
+def test_many_entries_in_many_rows(M, V, k, kind):
+    """Rows of one CTA and of a pair, on both sides of what their shared memory and the choice of kernel take of entries."""
+    case = _far(M, V, k, kind, 1.0, k)
+    loss, grad, loss1, grad1 = _calls(*case, 1.0)
+    _check(*case, 1.0, kind, loss, grad)
+    _check(*case, 1.0, kind, loss1, grad1)
+
+
 @pytest.mark.parametrize("rest", [False, True])
 @pytest.mark.parametrize("kind", ["fp16", "bf16", "fp32"])
 @pytest.mark.parametrize("M,V,k", [(4, 700, 5), (2, 40001, 64), (400, 1001, 7)])
