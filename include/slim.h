@@ -463,8 +463,8 @@ int slim_fp8_linear(const void* x, int x_type, long long ldx, const void* codes,
  *   saved   fp32 [M][4], 16-byte aligned: what _grad needs of _loss (same logits, entries, teacher_lse and temperature); may be NULL in _loss
  *   grad    [M][V] of the logits' type, row stride ldg >= V; may be the logits themselves (same pointer and stride); one that shares memory with them otherwise
  *           is refused.  No output may lie over another argument.
- * _step is _loss and _grad in one call: rows up to 65000 columns (half as many of fp32) are read once, longer ones a second
- * time, from L2 as a rule.  Sums over the columns in fp32, what is computed per entry in fp64; deterministic.
+ * _step is _loss and _grad in one call.  More rows than the GPU takes at once are read once up to 65000 columns (half as many of fp32) and 300 entries (160 of
+ * fp32 beyond 16000 columns); longer ones, and those with more entries, may be read a second time, from L2 as a rule.  Sums over the columns in fp32, what is computed per entry in fp64; deterministic.
  * 1 <= k <= SLIM_DISTILL_MAX_K, V <= SLIM_DISTILL_MAX_V, temperature > 0.  A device-side wait of the many-rows kernels that gives up leaves NaN
  * in the losses of the rows left undone. */
 #define SLIM_DISTILL_MAX_K 1024

@@ -6,16 +6,18 @@
 //     loss   = sum_j q_j (log q_j - log p_{i_j})   [ + q' (log q' - log p') ],   q' = 1 - sum_j q_j, p' = 1 - sum of p over the set
 //     dloss/ds_v = (p_v * c - sum_{j: i_j = v} q_j) / T
 // without the rest q_j is the softmax over the entries and c = sum_j q_j; with it q_j = exp(u_j / T - lse), and c is
-// sum_j q_j + q' for the listed columns, that less q' / p' for all others.  So a row needs its maximum, its sum of exponentials
-// outside the listed columns, and k logits; then its gradient is one multiplication per element and k corrections.
+// sum_j q_j + q' for the listed columns, that less q' / p' for all others.  So a row needs its sum of exponentials (with the rest, that outside the listed
+// columns, relative to the largest logit there, however far below the listed ones that lies) and k logits; then its gradient is one
+// multiplication per element and k corrections.
 //
 // Bound: HBM (a row is read once, its gradient written once), with two ex2 per element next to it.  Two kernels: a CTA or cluster per row, and
 // one that takes row after row (below).  A row belongs to 1 to 8 CTAs of 512 threads, each with a slice of its columns; a thread takes eight 16-byte
 // vectors of it at a time and, in the one call for both, keeps them in registers between the statistics and the gradient; a longer row is read a second
 // time, from L2.  The slices' statistics meet through distributed shared memory; every sum has a fixed order.  Sums over the columns are fp32, what is
 // computed of the entries, and the loss, is fp64, because a small loss is the difference of large terms.
-// Measured: loss of 512 x 152064 bf16 45 us, its gradient 57 (5.5 TB/s), both in one call 88; 777 x 50257 fp32 in one call 74, 4096 x 32000 bf16 131;
-// loss of 16 x 32000 8.2, all of it latency.
+// Measured: loss of 512 x 152064 bf16 45 us, its gradient 55 (5.7 TB/s), both in one call 88; 777 x 50257 fp32 in one call 74, 4096 x 32000 bf16 126;
+// loss of 16 x 32000 8.1, all of it latency.  Registers are held to two CTAs per SM (64 a thread, 56 in the many-rows kernel); what does not fit, up to 48 bytes a
+// thread of a row's terms and addresses, is read back a few times per row.
 #include "slim_exp.cuh"
 #include "slim_gemv_i8.cuh"
 

@@ -333,7 +333,8 @@ fp8_few_kernel(const __grid_constant__ CUtensorMap w_map, const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------ host side
-// Cut of a tile's K over c CTAs: time in blocks of 128 columns, of which a CTA's start and end cost about four.
+// Cut of a tile's K over c CTAs: time in blocks of 128 columns, of which a CTA's start and end cost about four.  It compares cuts of one call; what is the same
+// in all of them (launches, quantizer) does not count here, but does in fp8_few_cycles, which stands against another kernel's time.
 static int few_cluster(long long tiles, int G, int slots) {
     int best = 1;
     double least = 1e30;

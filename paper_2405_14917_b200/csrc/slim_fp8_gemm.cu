@@ -15,7 +15,8 @@
 // registers at once, so that the next tile's MMAs wait for the reading alone, and convert and store beside them.
 // Measured, call after call at the power cap, the quantizer of x among it: 2048 x 13824 x 5120 139 us (2.1 PFLOP/s at 1.25 GHz), 512 x 5120 x 13824 46,
 // 1000 x 4096 x 32000 137.
-// Persistent pairs; every wait is bounded and reports through the workspace status word.
+// Persistent pairs; every wait is bounded and reports through the workspace status word.  Compiled for 128 registers, as before the split, 100 bytes a thread
+// are spilled (the output warps alone hold 128 sums each, once a tile).
 #include "slim_fp8.cuh"
 
 #include <atomic>
