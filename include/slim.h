@@ -456,8 +456,8 @@ int slim_fp8_linear(const void* x, int x_type, long long ldx, const void* codes,
  * An entry whose index lies outside [0, V) is absent (padding: -1).  A row without a present entry, or (teacher_lse == NULL)
  * whose present values are all minus infinity, has loss 0 and gradient 0, whatever its logits.  An index that occurs
  * twice in a row is two entries of one column.  Logits of minus infinity have p = 0: with q > 0 there the loss is +infinity
- * and the gradient finite; where the columns outside the entries have p' = 0 and q' > 0 their gradient is 0.  NaN, and
- * logits of plus infinity, give NaN in their row alone.
+ * and the gradient finite; where all columns outside the entries are at minus infinity and q' > 0 their gradient is
+ * 0.  (Of finite logits p' is never 0, however small: loss and gradient are those of the formulas.)  NaN, and logits of plus infinity, give NaN in their row alone.
  *   logits  [M][V], row stride ld >= V elements, of SLIM_F32, SLIM_F16 or SLIM_BF16 (aligned to an element)
  *   index   int32 or int64 (index_bytes 4 or 8) [M][k]; value [M][k] of any of the three types; teacher_lse, dloss, loss fp32 [M]
  *   saved   fp32 [M][4], 16-byte aligned: what _grad needs of _loss (same logits, entries, teacher_lse and temperature); may be NULL in _loss
